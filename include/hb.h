@@ -79,6 +79,21 @@ typedef void *hb_stream;      /* hipStream_t */
 #define HB_MAX_TAPS_FIR1D 256   /* hb_fir1d: the large-tap regime of Sec. V-A */
 #define HB_MAX_TAPS_CONV2D 32   /* per axis, hb_conv2d, hb_down2, hb_up2 */
 #define HB_RESIZE_MAX_SPAN 512   /* hb_resize: largest band */
+#define HB_LINEAR_MAX_PITCH (1 << 21)   /* hb_linear: elements between two rows */
+#define HB_ATTENTION_MAX_D 128   /* hb_attention: channels of a head */
+#define HB_ROPE_MAX_AXES 4       /* hb_rope_axes */
+
+/* Element types of hb_linear's output and residual. */
+typedef enum { HB_F16 = 0, HB_F32 = 1 } hb_type;
+
+/* Activations of hb_linear. */
+typedef enum {
+    HB_ACT_NONE = 0,
+    HB_ACT_RELU = 1,          /* max(v, 0) */
+    HB_ACT_GELU = 2,          /* v (1 + erf(v / sqrt 2)) / 2 */
+    HB_ACT_GELU_TANH = 3,     /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
+    HB_ACT_SILU = 4           /* v / (1 + exp(-v)) */
+} hb_act;
 
 /* Human-readable name of a status code (static storage). */
 const char *hb_status_string(hb_status s);
@@ -366,6 +381,76 @@ hb_status hb_pyr_level(const hb_half *in, float *residual, hb_half *down_or_null
 hb_status hb_pyr_level_valu(const hb_half *in, float *residual, hb_half *down_or_null,
                             int H, int W, int64_t in_pitch, int64_t res_pitch, int64_t down_pitch,
                             hb_stream stream);
+
+/*
+ * Token operators.  What turns the pixels of a feature map (hb_conv3x3) into tokens and lets them look at the states of an
+ * encoder: a matrix product with its epilogue, rotary positions on several axes, attention to states of another length.
+ * Forward passes, like every stage here.  The conventions above hold (device pointers, one stream, no allocation, no
+ * synchronisation, validated before any HIP call); all sums, softmax statistics and angles are fp32.
+ *
+ * Matrix product with bias, activation and residual (a 1x1 convolution over NHWC pixels, a projection, a layer of an MLP):
+ *     out[m][n] = act(sum_{k < K} x[m][k] w[n][k] + bias[n]) + residual[m][n]
+ * x: M x K fp16, w: N x K fp16, bias: N fp16 or NULL, residual and out: M x N of out_type, residual may be NULL or `out`
+ * itself with its pitch (in place).  The sum, the bias, the activation and the residual are fp32 and rounded once, to
+ * out_type.  M, N, K >= 1; pitches in elements, >= the row, at most HB_LINEAR_MAX_PITCH (HB_ERR_UNSUPPORTED beyond; M times
+ * a pitch may pass 2^32).  Base pointers need the alignment of their elements; fastest with 16-byte aligned pointers and
+ * K and pitches that are multiples of 8.
+ * `workspace`: device scratch of at least hb_linear_workspace_size(M, N, K) bytes, 256-byte aligned, contents undefined on
+ * exit; concurrent calls need their own.  The size is 0, and the pointer may be NULL, where the sum over k is not split.
+ */
+size_t hb_linear_workspace_size(int M, int N, int K);
+hb_status hb_linear(const hb_half *x, const hb_half *w, const hb_half *bias_or_null, const void *residual_or_null, void *out,
+                    hb_type out_type, hb_act act, int M, int N, int K, int64_t x_pitch, int64_t w_pitch, int64_t residual_pitch,
+                    int64_t out_pitch, void *workspace, size_t workspace_bytes, hb_stream stream);
+hb_status hb_linear_valu(const hb_half *x, const hb_half *w, const hb_half *bias_or_null, const void *residual_or_null, void *out,
+                         hb_type out_type, hb_act act, int M, int N, int K, int64_t x_pitch, int64_t w_pitch, int64_t residual_pitch,
+                         int64_t out_pitch, void *workspace, size_t workspace_bytes, hb_stream stream);
+
+/*
+ * Rotary positions with several axes (row and column of an image, time, row and column of a video).  A token has one position per
+ * axis; P = sum of sections[a] pairs of channels turn, the first sections[0] of them with axis 0, the next sections[1] with
+ * axis 1 and so on, and channels from 2 P on are copied:
+ *     t = positions[b][l][axis of p] * freq[p]
+ *     (u, v) -> (u cos t - v sin t, v cos t + u sin t)
+ * Pair p is channels (p, P + p), or (2p, 2p + 1) where `interleaved` is not 0.  Negated frequencies turn back (the
+ * transpose, which is also the gradient).  x, out: B x L x H x D fp16, the last axis dense, the others with strides in elements;
+ * out may be x itself with its strides (in place).  positions: int32, positions[b * pos_batch + l * pos_token + a], pos_batch 0
+ * shares them between batches.  freq: P fp32 values, DEVICE memory.  sections: `axes` values, HOST memory, read before the
+ * call returns; 1 <= axes <= HB_ROPE_MAX_AXES, sections[a] >= 0, 1 <= P <= D / 2.  B, L, H >= 1, 2 <= D <= 65536.
+ * The angle is reduced to one turn before it is rounded: its error is about 2^-24 of a turn at positions up to 2^24 and
+ * 2^-19 at 2^31, beside that of freq itself.
+ * Fastest with 16-byte aligned rows (pointers and strides multiples of 8 elements, P a multiple of 8, or of 4 for interleaved).
+ */
+hb_status hb_rope_axes(const hb_half *x, hb_half *out, const int32_t *positions, const float *freq, int B, int L, int H, int D,
+                       int64_t x_batch, int64_t x_token, int64_t x_head, int64_t out_batch, int64_t out_token, int64_t out_head,
+                       int64_t pos_batch, int64_t pos_token, const int32_t *sections_host, int axes, int interleaved,
+                       hb_stream stream);
+
+/*
+ * Attention of Lq queries to the Lk states of an encoder, grouped heads (query head h reads key head h / (Hq / Hkv)):
+ *     s[j] = scale * sum_d q[b][i][h][d] k[b][j][h'][d]        for the visible keys j
+ *     out[b][i][h][d] = sum_j exp(s[j] - max s) v[b][j][h'][d] / sum_j exp(s[j] - max s)
+ * Key j of batch b is visible if j < key_len[b] (key_len may be NULL; values are clamped to 0 .. Lk) and key_mask[b *
+ * mask_pitch + j] is not 0 (key_mask may be NULL).  What stands in k and v at a key that is not visible, infinities and NaN
+ * included, has no influence; a row without a visible key is zero.  Lk may be 0.
+ * q, out: B x Lq x Hq x D fp16, k, v: B x Lk x Hkv x D fp16, the last axis dense, the others with strides in elements, any order;
+ * Hq a multiple of Hkv, D a multiple of 8, at most HB_ATTENTION_MAX_D (HB_ERR_UNSUPPORTED otherwise).  All strides multiples of 8
+ * and pointers 16-byte aligned; token strides of k and v at most 2^20 (HB_ERR_UNSUPPORTED beyond; other offsets may pass 2^32).
+ * Scores, maximum and sum are fp32; the weights exp(s - max) are rounded to fp16 for the product with v.
+ * `workspace`: device scratch of at least hb_attention_workspace_size(...) bytes, 256-byte aligned, contents undefined on
+ * exit; concurrent calls need their own.  The size is 0, and the pointer may be NULL, where the keys are not split.
+ */
+size_t hb_attention_workspace_size(int B, int Lq, int Lk, int Hq, int Hkv, int D);
+hb_status hb_attention(const hb_half *q, const hb_half *k, const hb_half *v, hb_half *out, int B, int Lq, int Lk, int Hq, int Hkv, int D,
+                       int64_t q_batch, int64_t q_token, int64_t q_head, int64_t k_batch, int64_t k_token, int64_t k_head,
+                       int64_t v_batch, int64_t v_token, int64_t v_head, int64_t out_batch, int64_t out_token, int64_t out_head,
+                       float scale, const int32_t *key_len_or_null, const uint8_t *key_mask_or_null, int64_t mask_pitch,
+                       void *workspace, size_t workspace_bytes, hb_stream stream);
+hb_status hb_attention_valu(const hb_half *q, const hb_half *k, const hb_half *v, hb_half *out, int B, int Lq, int Lk, int Hq, int Hkv, int D,
+                            int64_t q_batch, int64_t q_token, int64_t q_head, int64_t k_batch, int64_t k_token, int64_t k_head,
+                            int64_t v_batch, int64_t v_token, int64_t v_head, int64_t out_batch, int64_t out_token, int64_t out_head,
+                            float scale, const int32_t *key_len_or_null, const uint8_t *key_mask_or_null, int64_t mask_pitch,
+                            void *workspace, size_t workspace_bytes, hb_stream stream);
 
 /*
  * Measurement helper, not a stage: out[i] = (float) in[i] for n elements with 16-byte

@@ -326,3 +326,70 @@ def pyr_level(img, want_down: bool = False):
     _load().hbo_pyr_level(pi, _f64(res), _f64(down) if want_down else None,
                           H, W, W, W, W // 2)
     return (res, down) if want_down else res
+
+
+# ---- token operators: fp64 in numpy, straight from the definitions ----------------------------------------
+
+_SQRT2_PI = float(np.sqrt(2.0 / np.pi))
+
+
+def activation(v, act):
+    """none, relu, gelu (by the error function), gelu_tanh, silu of float64 values."""
+    v = np.asarray(v, dtype=np.float64)
+    if act == "relu":
+        return np.maximum(v, 0.0)
+    if act == "gelu":
+        from math import erfc
+        return 0.5 * v * np.vectorize(erfc, otypes=[np.float64])(-v / np.sqrt(2.0))
+    if act == "gelu_tanh":
+        return 0.5 * v * (1.0 + np.tanh(_SQRT2_PI * (v + 0.044715 * v ** 3)))
+    if act == "silu":
+        with np.errstate(over="ignore"):
+            return v / (1.0 + np.exp(-v))
+    assert act == "none"
+    return v
+
+
+def linear(x, w, bias=None, residual=None, act="none"):
+    """out[m][n] = act(sum_k x[m][k] w[n][k] + bias[n]) + residual[m][n] on float64 arrays."""
+    v = np.asarray(x, dtype=np.float64) @ np.asarray(w, dtype=np.float64).T
+    if bias is not None:
+        v = v + bias[None, :]
+    v = activation(v, act)
+    return v if residual is None else v + residual
+
+
+def rope_axes(x, positions, freq, sections, interleaved):
+    """Channel pairs of x[b][l][h][:] turned by positions[b][l][axis of the pair] * freq[pair]."""
+    x = np.asarray(x, dtype=np.float64)
+    out = x.copy()
+    pairs = int(sum(sections))
+    p = 0
+    for axis, n in enumerate(sections):
+        for _ in range(n):
+            u, v = (2 * p, 2 * p + 1) if interleaved else (p, pairs + p)
+            t = positions[:, :, axis].astype(np.float64)[:, :, None] * float(freq[p])
+            out[..., u] = x[..., u] * np.cos(t) - x[..., v] * np.sin(t)
+            out[..., v] = x[..., v] * np.cos(t) + x[..., u] * np.sin(t)
+            p += 1
+    return out
+
+
+def attention(q, k, v, scale, key_len=None, key_mask=None):
+    """softmax(scale q k^T) v over the visible keys, a row without any is zero; q [B, Lq, Hq, D], k and v [B, Lk, Hkv, D].  A key
+    that is not visible is left out before anything is computed."""
+    q, k, v = (np.asarray(t, dtype=np.float64) for t in (q, k, v))
+    B, Lq, Hq, D = q.shape
+    Lk, Hkv = k.shape[1], k.shape[2]
+    out = np.zeros((B, Lq, Hq, D))
+    for b in range(B):
+        n = Lk if key_len is None else min(max(int(key_len[b]), 0), Lk)
+        seen = [j for j in range(n) if key_mask is None or key_mask[b, j]]
+        if not seen:
+            continue
+        for h in range(Hq):
+            hk = h // (Hq // Hkv)
+            s = scale * (q[b, :, h] @ k[b, seen, hk].T)
+            e = np.exp(s - s.max(axis=1, keepdims=True))
+            out[b, :, h] = (e @ v[b, seen, hk]) / e.sum(axis=1, keepdims=True)
+    return out

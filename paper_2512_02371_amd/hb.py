@@ -28,6 +28,10 @@ HB_ERR_HIP = 4
 HB_MAX_TAPS = 64            # per axis, hb_sepblur
 HB_MAX_TAPS_FIR1D = 256     # hb_fir1d
 HB_MAX_TAPS_CONV2D = 32     # per axis, hb_conv2d
+HB_LINEAR_MAX_PITCH = 1 << 21
+HB_ATTENTION_MAX_D = 128
+HB_ROPE_MAX_AXES = 4
+HB_ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}      # hb_linear
 
 # every symbol include/hb.h declares
 SYMBOLS = [
@@ -42,6 +46,9 @@ SYMBOLS = [
     "hb_sat2d_workspace_size", "hb_sat2d", "hb_sat2d_valu", "hb_sat2d_noalloc", "hb_sat2d_set_wait_limit",
     "hb_conv3x3", "hb_conv3x3_valu",
     "hb_pyr_level", "hb_pyr_level_valu",
+    "hb_linear_workspace_size", "hb_linear", "hb_linear_valu",
+    "hb_rope_axes",
+    "hb_attention_workspace_size", "hb_attention", "hb_attention_valu",
     "hb_copy_f16_f32", "hb_mfma_probe",
 ]
 
@@ -112,6 +119,17 @@ def load() -> ctypes.CDLL:
     L.hb_sat2d_set_wait_limit.restype = I
     L.hb_sat2d_workspace_size.argtypes = [I, I]
     L.hb_sat2d_workspace_size.restype = ctypes.c_size_t
+    lin = [vp, vp, vp, vp, vp, I, I, I, I, I, I64, I64, I64, I64, vp, ctypes.c_size_t, vp]
+    att = [vp, vp, vp, vp, I, I, I, I, I, I] + [I64] * 12 + [ctypes.c_float, vp, vp, I64, vp, ctypes.c_size_t, vp]
+    for name, sig in (("hb_linear", lin), ("hb_linear_valu", lin), ("hb_attention", att), ("hb_attention_valu", att),
+                      ("hb_rope_axes", [vp, vp, vp, vp, I, I, I, I] + [I64] * 8 + [vp, I, I, vp])):
+        f = getattr(L, name)
+        f.argtypes = sig
+        f.restype = I
+    for name, n in (("hb_linear_workspace_size", 3), ("hb_attention_workspace_size", 6)):
+        f = getattr(L, name)
+        f.argtypes = [I] * n
+        f.restype = ctypes.c_size_t
     _lib = L
     # built against one torch: with another, or not built at all, it does not load, and ctypes makes every call
     try:
@@ -452,6 +470,106 @@ def hb_pyr_level(inp, residual, down=None):
 
 def hb_pyr_level_valu(inp, residual, down=None):
     return _pyr("hb_pyr_level_valu", inp, residual, down)
+
+
+def hb_linear_workspace_size(M, N, K):
+    return int(load().hb_linear_workspace_size(int(M), int(N), int(K)))
+
+
+def _scratch(t):
+    """Address and size of a workspace; None is none."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous(), "contiguous uint8 CUDA tensor expected"
+    return t.data_ptr(), t.numel()
+
+
+def _linear(name, x, w, out, workspace, bias, residual, act):
+    px, M, K, xp = _img2d(x, torch.float16)
+    pw, N, Kw, wp = _img2d(w, torch.float16)
+    assert out.dtype in (torch.float16, torch.float32), "fp16 or fp32 output expected"
+    po, Mo, No, op = _img2d(out, out.dtype)
+    assert K == Kw and (Mo, No) == (M, N), "x: M x K, w: N x K, out: M x N"
+    pb = pr = None
+    rp = N
+    if bias is not None:
+        assert bias.is_cuda and bias.dtype == torch.float16 and bias.shape == (N,) and bias.is_contiguous(), "bias: N"
+        pb = bias.data_ptr()
+    if residual is not None:
+        pr, Mr, Nr, rp = _img2d(residual, out.dtype)
+        assert (Mr, Nr) == (M, N), "residual: M x N"
+    pws, nws = _scratch(workspace)
+    if M == 1:                                    # the pitch of a single row has no meaning, and torch gives any
+        xp, op, rp = K, N, N
+    if N == 1:
+        wp = K
+    _check(name, getattr(_lib or load(), name)(px, pw, pb, pr, po, 1 if out.dtype == torch.float32 else 0, HB_ACTS[act], M, N, K, xp, wp, rp, op,
+                                               pws, nws, _stream()))
+    return out
+
+
+def hb_linear(x, w, out, workspace=None, bias=None, residual=None, act="none"):
+    """out = act(x w^T + bias) + residual; x: M x K, w: N x K, out and residual: M x N, fp16 or fp32."""
+    return _linear("hb_linear", x, w, out, workspace, bias, residual, act)
+
+
+def hb_linear_valu(x, w, out, workspace=None, bias=None, residual=None, act="none"):
+    return _linear("hb_linear_valu", x, w, out, workspace, bias, residual, act)
+
+
+def _heads(t):
+    """B x L x H x D, the last axis dense -> (address, (B, L, H, D), strides of the first three)."""
+    s = t.stride()
+    assert t.is_cuda and t.dtype == torch.float16 and len(s) == 4 and (s[3] == 1 or t.shape[3] == 1), "B x L x H x D fp16 CUDA tensor expected"
+    return t.data_ptr(), t.shape, s[:3]
+
+
+def hb_rope_axes(x, out, positions, freq, sections, interleaved=False):
+    """Turns channel pairs of x (B x L x H x D) by positions (B x L x axes) times freq; out may be x."""
+    px, (B, L, H, D), xs = _heads(x)
+    po, shape, os_ = _heads(out)
+    assert shape == x.shape, "output shape"
+    n = len(sections)
+    ps = positions.stride()
+    assert positions.is_cuda and positions.dtype == torch.int32 and tuple(positions.shape) == (B, L, n) and (ps[2] == 1 or n == 1), "positions: B x L x axes, int32"
+    assert freq.is_cuda and freq.dtype == torch.float32 and freq.is_contiguous() and freq.shape == (sum(sections),), "freq: a value per pair, fp32"
+    _check("hb_rope_axes", (_lib or load()).hb_rope_axes(px, po, positions.data_ptr(), freq.data_ptr(), B, L, H, D, *xs, *os_, ps[0], ps[1],
+                                                         (ctypes.c_int32 * n)(*sections), n, int(bool(interleaved)), _stream()))
+    return out
+
+
+def hb_attention_workspace_size(B, Lq, Lk, Hq, Hkv, D):
+    return int(load().hb_attention_workspace_size(int(B), int(Lq), int(Lk), int(Hq), int(Hkv), int(D)))
+
+
+def _attention(name, q, k, v, out, scale, workspace, key_len, key_mask):
+    pq, (B, Lq, Hq, D), qs = _heads(q)
+    pk, (Bk, Lk, Hkv, Dk), ks = _heads(k)
+    pv, shape, vs = _heads(v)
+    po, oshape, os_ = _heads(out)
+    assert (Bk, Dk) == (B, D) and shape == k.shape and oshape == q.shape, "q, out: B x Lq x Hq x D, k, v: B x Lk x Hkv x D"
+    pl = pm = None
+    mp = 0
+    if key_len is not None:
+        assert key_len.is_cuda and key_len.dtype == torch.int32 and key_len.shape == (B,) and key_len.is_contiguous(), "key_len: B, int32"
+        pl = key_len.data_ptr()
+    if key_mask is not None:
+        assert key_mask.is_cuda and key_mask.dtype in (torch.uint8, torch.bool) and key_mask.shape == (B, Lk), "key_mask: B x Lk, uint8 or bool"
+        assert key_mask.stride(1) == 1 or Lk <= 1, "key_mask: dense rows"
+        pm, mp = key_mask.data_ptr(), key_mask.stride(0)
+    pws, nws = _scratch(workspace)
+    _check(name, getattr(_lib or load(), name)(pq, pk, pv, po, B, Lq, Lk, Hq, Hkv, D, *qs, *ks, *vs, *os_, float(scale), pl, pm, mp,
+                                               pws, nws, _stream()))
+    return out
+
+
+def hb_attention(q, k, v, out, scale, workspace=None, key_len=None, key_mask=None):
+    """out = softmax(scale q k^T) v over the visible keys; q, out: B x Lq x Hq x D, k, v: B x Lk x Hkv x D."""
+    return _attention("hb_attention", q, k, v, out, scale, workspace, key_len, key_mask)
+
+
+def hb_attention_valu(q, k, v, out, scale, workspace=None, key_len=None, key_mask=None):
+    return _attention("hb_attention_valu", q, k, v, out, scale, workspace, key_len, key_mask)
 
 
 def hb_copy_f16_f32(inp, out):
