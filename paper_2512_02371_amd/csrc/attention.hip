@@ -2,8 +2,10 @@
 #include <float.h>
 #include <math.h>
 
+#include "attention_plan.hpp"
 #include "hb_device.hpp"
 #include "hb_host.hpp"
+#include "token_tiles.hpp"
 
 namespace hb {
 
@@ -15,10 +17,13 @@ struct AttentionArgs {
     int B, Lq, Lk, Hq, Hkv, D;
     int group;                 // query heads per key head
     int64_t q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head, out_batch, out_token, out_head;
-    float scale2;              // scale * log2(e): the weights are powers of two
+    float scale2;              // |scale| * log2(e): the weights are powers of two
+    bool negate;               // scale < 0: the queries' sign
     const int32_t* key_len;    // null: all
     const uint8_t* key_mask;   // null: all
     int64_t mask_pitch;
+    float* parts;              // keys split: sums of the parts, [part][row][D], then their maximum and sum of weights, [part][row][2]
+    int nparts;
 };
 
 __device__ __forceinline__ int attention_keys(const AttentionArgs& p, int b) { return p.key_len ? clampi(p.key_len[b], 0, p.Lk) : p.Lk; }
@@ -36,6 +41,7 @@ __global__ void __launch_bounds__(256) attention_valu_kernel(AttentionArgs p) {
     const half_t* v = p.v + b * p.v_batch + hk * p.v_head;
     const uint8_t* mask = p.key_mask ? p.key_mask + b * p.mask_pitch : nullptr;
     const int len = attention_keys(p, b);
+    const float scale2 = p.negate ? -p.scale2 : p.scale2;
     float top = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
     for (int j0 = 0; j0 < len; j0 += 64) {
         const int j = j0 + lane;
@@ -45,7 +51,7 @@ __global__ void __launch_bounds__(256) attention_valu_kernel(AttentionArgs p) {
             const half_t* kj = k + j * p.k_token;
             float dot = 0.f;
             for (int d = 0; d < p.D; ++d) dot = fmaf((float)q[d], (float)kj[d], dot);
-            s = dot * p.scale2;
+            s = dot * scale2;
         }
         const uint64_t any = __ballot(seen);
         if (!any) continue;
@@ -73,6 +79,246 @@ __global__ void __launch_bounds__(256) attention_valu_kernel(AttentionArgs p) {
     if (lane + 64 < p.D) o[lane + 64] = (half_t)(o1 * inv);
 }
 
+// ---------------------------------------------------------------------------
+// On the matrix units.  The query heads that share a key head are rows of one product: row r is query r / group of head r % group.
+//
+// A wave holds 32 rows, a workgroup of four waves shares the keys, 64 at a time.  With v_mfma_f32_32x32x16_f16 the scores are formed as
+// S^T = K Q^T, so that a lane (c, h) has 32 of the 64 scores of ONE row c (keys 8 q + 4 h + r of each 32): maximum and sum need one
+// exchange with lane c + 32, and the weights, rounded to fp16, are in place as the operand of O^T = V^T P^T, whose contraction runs
+// over the keys in the order that the lanes hold them.  V^T is read from LDS by transposing reads.
+constexpr int kAttRows = 32, kAttWaves = 4, kAttTile = kAttRows * kAttWaves;
+
+// A tile of keys in LDS: rows of PC 16-byte pieces (8 up to 64 channels, else 16), a piece at place piece ^ flip: what the fragments' reads
+// take at one time (16 rows of one piece of k; 4 rows of 64 bytes of v) lies in different banks.
+template <int PC>
+__device__ __forceinline__ int att_flip_k(int row) { return PC == 8 ? (row >> 1) & 7 : row & 15; }
+template <int PC>
+__device__ __forceinline__ int att_flip_v(int row) { return PC == 8 ? (row << 1) & 4 : (row << 2) & 12; }
+
+// D rounded up to DP; PARTS: the sums go to the workspace.
+template <int DP, bool PARTS>
+__global__ void __launch_bounds__(64 * kAttWaves, DP > 64 ? 2 : 3) attention_mfma_kernel(AttentionArgs p) {
+    constexpr int PC = DP <= 64 ? 8 : 16, kSteps = DP / 16, kBlocks = DP / 32;
+    constexpr int kPitch = 16 * PC, kMatrix = 64 * kPitch, kStage = 2 * kMatrix;      // bytes: a row, a tile of k or v, both
+    constexpr int kOwn = PC / 4, kRowsOf = 64 / PC;                                    // copies of 1 KB per matrix and wave, rows in one
+    constexpr int kOutPitch = 2 * DP + 16;                                             // bytes of a row on its way out
+    constexpr int kLds = 2 * kStage > kAttTile * kOutPitch ? 2 * kStage : kAttTile * kOutPitch;
+    __shared__ __attribute__((aligned(1024))) char s_tiles[kLds];
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 31, h = lane >> 5;
+
+    // neighbouring workgroups read the same keys
+    const int rows = p.Lq * p.group, tiles = (rows + kAttTile - 1) / kAttTile;
+    const int id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int tile = id % tiles, part = id / tiles % p.nparts, bh = id / tiles / p.nparts;
+    const int hk = bh % p.Hkv, b = bh / p.Hkv;
+    const int row0 = tile * kAttTile + wv * kAttRows;
+    const bool active = row0 < rows;
+
+    // this part's keys
+    const int len = attention_keys(p, b), all = (len + 63) >> 6;
+    const int first = (int)((int64_t)all * part / p.nparts), last = (int)((int64_t)all * (part + 1) / p.nparts);
+    const uint8_t* const mask = p.key_mask ? p.key_mask + b * p.mask_pitch : nullptr;
+
+    // queries: qf[s] lane (c, h) = channels 16 s + 8 h .. + 7 of row c
+    half8 qf[kSteps];
+    {
+        const int row = min(row0 + c, rows - 1), i = row / p.group, g = row - i * p.group;
+        const half_t* q = p.q + b * p.q_batch + i * p.q_token + (hk * p.group + g) * p.q_head + 8 * h;
+        const uint32_t turn = p.negate ? 0x80008000u : 0u;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            u32x4 v = {0, 0, 0, 0};
+            if (16 * s + 8 * h < p.D) v = *reinterpret_cast<const u32x4*>(q + 16 * s);
+            qf[s] = __builtin_bit_cast(half8, v ^ turn);
+        }
+    }
+
+    // copies of a tile: slot `lane` of copy i is row kRowsOf * i + lane / PC, place lane % PC
+    const char* const k0 = reinterpret_cast<const char*>(p.k + b * p.k_batch + hk * p.k_head);
+    const char* const v0 = reinterpret_cast<const char*>(p.v + b * p.v_batch + hk * p.v_head);
+    const uint32_t lds0 = tk_lds_addr(s_tiles);
+    auto seen_of = [&](int t, uint32_t byte) HB_INLINE {      // the visible keys of tile t; `byte` is a lane's key's mask
+        const int j = 64 * t + lane;
+        return __ballot(j < len && byte != 0);
+    };
+    auto byte_of = [&](int t) HB_INLINE {
+        const int j = 64 * t + lane;
+        return mask && j < len ? (uint32_t)mask[j] : 1u;
+    };
+    auto request = [&](int t, uint64_t seen, int buf) HB_INLINE {
+        const u32x4 rk = tk_rsrc(k0 + (int64_t)t * 128 * p.k_token), rv = tk_rsrc(v0 + (int64_t)t * 128 * p.v_token);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int row = kRowsOf * (kOwn * wv + i) + lane / PC, place = lane % PC;
+            const int ck = place ^ att_flip_k<PC>(row), cv = place ^ att_flip_v<PC>(row);
+            const bool there = (seen >> row) & 1;
+            const uint32_t to = lds0 + buf * kStage + 1024 * (kOwn * wv + i);
+            tk_dma16(rk, there && 8 * ck < p.D ? (uint32_t)row * (uint32_t)(2 * p.k_token) + 16 * ck : kTkOutside, 0, to);
+            tk_dma16(rv, there && 8 * cv < p.D ? (uint32_t)row * (uint32_t)(2 * p.v_token) + 16 * cv : kTkOutside, 0, to + kMatrix);
+        }
+    };
+
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    const uint32_t at_k = lds0 + c * kPitch + 16 * (h ^ att_flip_k<PC>(c));
+    const int vrow = 4 * h + ((lane & 15) >> 2);
+    const uint32_t at_v = lds0 + kMatrix + vrow * kPitch + ((16 * (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) ^ (16 * att_flip_v<PC>(vrow))) + 8 * (lane & 1);
+    auto read_k = [&](int block, int s, int buf) HB_INLINE {
+        return *reinterpret_cast<const __attribute__((address_space(3))) half8*>((at_k ^ (32 * s)) + buf * kStage + 32 * kPitch * block);
+    };
+    auto read_v = [&](int db, int key, int buf) HB_INLINE {   // 4 keys from `key` (+ 4 h) on of channel 32 db + c
+        return __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                             reinterpret_cast<__attribute__((address_space(3))) short4v*>((at_v ^ (64 * db)) + buf * kStage + key * kPitch)));
+    };
+
+    floatx16 o[kBlocks];
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    float top = -INFINITY, base = 0.f, sum = 0.f;             // this row's largest score, or up to 8 less, and this lane's sum of weights
+    bool far = false;                                         // scores beyond 2^13
+
+    uint64_t seen = 0;
+    uint32_t byte = 0;
+    if (first < last) {
+        seen = seen_of(first, byte_of(first));
+        request(first, seen, 0);
+        byte = byte_of(min(first + 1, last - 1));
+    }
+    for (int t = first; t < last; ++t) {
+        const int buf = (t - first) & 1;
+        const uint64_t next = t + 1 < last ? seen_of(t + 1, byte) : 0;
+        tk_wait_loads<0>();
+        lds_barrier();
+        if (t + 1 < last) {
+            request(t + 1, next, buf ^ 1);
+            byte = byte_of(min(t + 2, last - 1));
+        }
+        if (active && seen) {
+            floatx16 s[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[k][j] = 0.f;
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) s[k] = mfma32x32x16(read_k(k, i, buf), qf[i], s[k]);
+            }
+            if (~seen) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t bits = (uint32_t)(seen >> (32 * k)) >> (4 * h);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) s[k][j] = (bits >> (8 * (j / 4) + j % 4)) & 1 ? s[k][j] : -INFINITY;
+                }
+            }
+            float most = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+            for (int j = 1; j < 16; ++j) most = fmaxf(most, fmaxf(s[0][j], s[1][j]));
+            most = fmaxf(most, __shfl_xor(most, 32)) * p.scale2;
+            // Weights are 2^7 at the maximum that they refer to: fp16 then holds those down to 2^-21 of it in full, and up to 2^8 more is
+            // as good, so that the sums are moved only where the maximum grows by more than that.
+            if (__any(most > top + 8.f)) {
+                const float before = top;
+                top = fmaxf(top, most);
+                base = top == -INFINITY ? 0.f : top - 7.f;
+                const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(before - top);
+                sum *= keep;
+#pragma unroll
+                for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[i][j] *= keep;
+                far = __any(fabsf(base) > 8192.f);
+            }
+            half8 w[4];
+            if (!far) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) w[j / 8][j % 8] = (half_t)__builtin_amdgcn_exp2f(fmaf(s[j / 16][j % 16], p.scale2, -base));
+            } else {                                          // the rounding of a product that large would show: the same product for maximum and score
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    float x = s[j / 16][j % 16] * p.scale2;
+                    asm volatile("" : "+v"(x));
+                    w[j / 8][j % 8] = (half_t)__builtin_amdgcn_exp2f(x - base);
+                }
+            }
+            typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+            const half2v ones = {1, 1};
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum = __builtin_amdgcn_fdot2(half2v{w[j / 4][2 * (j % 4)], w[j / 4][2 * (j % 4) + 1]}, ones, sum, false);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < kBlocks; ++i) o[i] = mfma32x32x16(join(read_v(i, 16 * k, buf), read_v(i, 16 * k + 8, buf)), w[k], o[i]);
+        }
+        seen = next;
+    }
+    sum += __shfl_xor(sum, 32);
+    if (PARTS) {
+        if (active && row0 + c < rows) {
+            const int64_t total = (int64_t)p.B * p.Hkv * rows, at = part * total + (int64_t)bh * rows + row0 + c;
+            float* to = p.parts + at * p.D + 4 * h;
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (32 * i + 8 * q < p.D) *reinterpret_cast<floatx4*>(to + 32 * i + 8 * q) = floatx4{o[i][4 * q], o[i][4 * q + 1], o[i][4 * q + 2], o[i][4 * q + 3]};
+            if (h == 0) {
+                float* ml = p.parts + p.nparts * total * p.D + 2 * at;
+                ml[0] = top;
+                ml[1] = sum;
+            }
+        }
+        return;
+    }
+    // out: through LDS, whole rows
+    lds_barrier();
+    if (!active) return;
+    char* const patch = s_tiles + wv * kAttRows * kOutPitch;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<half4*>(patch + c * kOutPitch + 2 * (32 * i + 8 * q + 4 * h)) =
+                to_half4(floatx4{o[i][4 * q], o[i][4 * q + 1], o[i][4 * q + 2], o[i][4 * q + 3]} * inv);
+    wave_lds_fence();
+    constexpr int kLanes = DP / 8 <= 8 ? 8 : 16;
+    const int piece = lane % kLanes;
+#pragma unroll
+    for (int r = lane / kLanes; r < kAttRows; r += 64 / kLanes) {
+        const int row = row0 + r, i = row / p.group, g = row - i * p.group;
+        if (row < rows && 8 * piece < p.D)
+            *reinterpret_cast<half8*>(p.out + b * p.out_batch + i * p.out_token + (hk * p.group + g) * p.out_head + 8 * piece) =
+                *reinterpret_cast<const half8*>(patch + r * kOutPitch + 16 * piece);
+    }
+}
+
+// The parts' sums of a row brought to their common maximum, in their order; a thread per four channels.
+__global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs p) {
+    const int per = p.D / 4, rows = p.Lq * p.group;
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, at = t / per, total = (int64_t)p.B * p.Hkv * rows;
+    if (at >= total) return;
+    const int d = (int)(t - at * per) * 4;
+    const float *o = p.parts + at * p.D + d, *ml = p.parts + p.nparts * total * p.D + 2 * at;
+    float top = -INFINITY;
+    for (int s = 0; s < p.nparts; ++s) top = fmaxf(top, ml[2 * s * total]);
+    const float base = top == -INFINITY ? 0.f : top;
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < p.nparts; ++s) {
+        const float w = __builtin_amdgcn_exp2f(ml[2 * s * total] - base);
+        sum += w * ml[2 * s * total + 1];
+        const floatx4 q = *reinterpret_cast<const floatx4*>(o + s * total * p.D);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += w * q[i];
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int bh = (int)(at / rows), row = (int)(at - (int64_t)bh * rows), i = row / p.group, g = row - i * p.group, b = bh / p.Hkv, hk = bh - b * p.Hkv;
+    *reinterpret_cast<half4*>(p.out + b * p.out_batch + i * p.out_token + (hk * p.group + g) * p.out_head + d) = to_half4(v * inv);
+}
+
 static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_half* k, const hb_half* v, hb_half* out, int B, int Lq, int Lk,
                                    int Hq, int Hkv, int D, const int64_t (&st)[12], float scale, const int32_t* key_len,
                                    const uint8_t* key_mask, int64_t mask_pitch) {
@@ -85,11 +331,24 @@ static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_
         if (s < 0 || s % 8 != 0) return HB_ERR_INVALID_ARG;
     if (key_mask && mask_pitch < 0) return HB_ERR_INVALID_ARG;
     if (D % 8 != 0 || D > HB_ATTENTION_MAX_D) return HB_ERR_UNSUPPORTED;
-    if (st[4] > (1 << 20) || st[7] > (1 << 20)) return HB_ERR_UNSUPPORTED;
+    if (st[4] > (1 << 20) || st[7] > (1 << 20) || (int64_t)Lq * (Hq / Hkv) > 0x7fffff00) return HB_ERR_UNSUPPORTED;
     a = {reinterpret_cast<const half_t*>(q), reinterpret_cast<const half_t*>(k), reinterpret_cast<const half_t*>(v), reinterpret_cast<half_t*>(out),
          B, Lq, Lk, Hq, Hkv, D, Hq / Hkv, st[0], st[1], st[2], st[3], st[4], st[5], st[6], st[7], st[8], st[9], st[10], st[11],
-         scale * 1.44269504f, key_len, key_mask, mask_pitch};
+         // a scale of 0 as one that is too small to tell: hidden scores are -inf, and that times 0 is no number
+         fmaxf(fabsf(scale) * 1.44269504f, 1e-30f), scale < 0.f, key_len, key_mask, mask_pitch, nullptr, 1};
     return HB_OK;
+}
+
+template <bool PARTS>
+static hb_status attention_run(const AttentionArgs& a, hipStream_t st) {
+    const int64_t wgs = (int64_t)a.B * a.Hkv * attention_tiles(a.Lq, a.group) * a.nparts;
+    if (wgs > 0x7fffffff) return HB_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)wgs), block(64 * kAttWaves);
+    if (a.D <= 32) hipLaunchKernelGGL((attention_mfma_kernel<32, PARTS>), grid, block, 0, st, a);
+    else if (a.D <= 64) hipLaunchKernelGGL((attention_mfma_kernel<64, PARTS>), grid, block, 0, st, a);
+    else if (a.D <= 96) hipLaunchKernelGGL((attention_mfma_kernel<96, PARTS>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((attention_mfma_kernel<128, PARTS>), grid, block, 0, st, a);
+    return launch_status();
 }
 
 }  // namespace hb
@@ -103,7 +362,10 @@ static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_
     attention_prepare(a, q, k, v, out, B, Lq, Lk, Hq, Hkv, D, {q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head, \
                       out_batch, out_token, out_head}, scale, key_len, key_mask, mask_pitch)
 
-extern "C" size_t hb_attention_workspace_size(int B, int Lq, int Lk, int Hq, int Hkv, int D) { return 0; }
+extern "C" size_t hb_attention_workspace_size(int B, int Lq, int Lk, int Hq, int Hkv, int D) {
+    if (B < 1 || Lq < 1 || Lk < 1 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv != 0 || (int64_t)Lq * (Hq / Hkv) > 0x7fffff00) return 0;
+    return hb::attention_workspace(B, Lq, Lk, Hq, Hkv, D);
+}
 
 extern "C" hb_status hb_attention_valu(HB_ATTENTION_PARAMS) {
     using namespace hb;
@@ -116,6 +378,18 @@ extern "C" hb_status hb_attention_valu(HB_ATTENTION_PARAMS) {
 }
 
 extern "C" hb_status hb_attention(HB_ATTENTION_PARAMS) {
-    return hb_attention_valu(q, k, v, out, B, Lq, Lk, Hq, Hkv, D, q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head,
-                             out_batch, out_token, out_head, scale, key_len, key_mask, mask_pitch, workspace, workspace_bytes, stream);
+    using namespace hb;
+    AttentionArgs a;
+    if (hb_status s = HB_ATTENTION_PREPARE(a)) return s;
+    const auto st = reinterpret_cast<hipStream_t>(stream);
+    if (const size_t need = attention_workspace(B, Lq, Lk, Hq, Hkv, D)) {
+        if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need) return HB_ERR_WORKSPACE;
+        a.nparts = attention_parts(B, Lq, Lk, Hq, Hkv);
+        a.parts = static_cast<float*>(workspace);
+        if (hb_status s = attention_run<true>(a, st)) return s;
+        const int64_t blocks = ((int64_t)B * Hq * Lq * (D / 4) + 255) / 256;
+        hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
+        return launch_status();
+    }
+    return attention_run<false>(a, st);
 }
