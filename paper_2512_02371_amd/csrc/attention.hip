@@ -142,33 +142,45 @@ __global__ void __launch_bounds__(64 * kAttWaves, DP > 64 ? 2 : 3) attention_mfm
         const int j = 64 * t + lane;
         return __ballot(j < len && byte != 0);
     };
-    auto byte_of = [&](int t) HB_INLINE {
-        const int j = 64 * t + lane;
-        return mask && j < len ? (uint32_t)mask[j] : 1u;
-    };
+    auto mask_of = [&](int t) HB_INLINE { return (uint32_t)mask[min(64 * t + lane, len - 1)]; };
+    uint32_t off_k[kOwn], off_v[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        const int row = kRowsOf * (kOwn * wv + i) + lane / PC, place = lane % PC;
+        const int ck = place ^ att_flip_k<PC>(row), cv = place ^ att_flip_v<PC>(row);
+        off_k[i] = 8 * ck < p.D ? (uint32_t)row * (uint32_t)(2 * p.k_token) + 16 * ck : kTkOutside;
+        off_v[i] = 8 * cv < p.D ? (uint32_t)row * (uint32_t)(2 * p.v_token) + 16 * cv : kTkOutside;
+    }
     auto request = [&](int t, uint64_t seen, int buf) HB_INLINE {
         const u32x4 rk = tk_rsrc(k0 + (int64_t)t * 128 * p.k_token), rv = tk_rsrc(v0 + (int64_t)t * 128 * p.v_token);
+        const uint32_t to = lds0 + buf * kStage + 1024 * kOwn * wv;
+        if (~seen == 0) {
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-            const int row = kRowsOf * (kOwn * wv + i) + lane / PC, place = lane % PC;
-            const int ck = place ^ att_flip_k<PC>(row), cv = place ^ att_flip_v<PC>(row);
-            const bool there = (seen >> row) & 1;
-            const uint32_t to = lds0 + buf * kStage + 1024 * (kOwn * wv + i);
-            tk_dma16(rk, there && 8 * ck < p.D ? (uint32_t)row * (uint32_t)(2 * p.k_token) + 16 * ck : kTkOutside, 0, to);
-            tk_dma16(rv, there && 8 * cv < p.D ? (uint32_t)row * (uint32_t)(2 * p.v_token) + 16 * cv : kTkOutside, 0, to + kMatrix);
+            for (int i = 0; i < kOwn; ++i) {
+                tk_dma16(rk, off_k[i], 0, to + 1024 * i);
+                tk_dma16(rv, off_v[i], 0, to + 1024 * i + kMatrix);
+            }
+        } else {                                              // what is hidden arrives as zeros
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                const bool there = (seen >> (kRowsOf * (kOwn * wv + i) + lane / PC)) & 1;
+                tk_dma16(rk, there ? off_k[i] : kTkOutside, 0, to + 1024 * i);
+                tk_dma16(rv, there ? off_v[i] : kTkOutside, 0, to + 1024 * i + kMatrix);
+            }
         }
     };
 
     typedef short short4v __attribute__((ext_vector_type(4)));
-    const uint32_t at_k = lds0 + c * kPitch + 16 * (h ^ att_flip_k<PC>(c));
+    uint32_t at_k[kSteps], at_v[kBlocks];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) at_k[i] = lds0 + c * kPitch + ((16 * (h ^ att_flip_k<PC>(c))) ^ (32 * i));
     const int vrow = 4 * h + ((lane & 15) >> 2);
-    const uint32_t at_v = lds0 + kMatrix + vrow * kPitch + ((16 * (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) ^ (16 * att_flip_v<PC>(vrow))) + 8 * (lane & 1);
-    auto read_k = [&](int block, int s, int buf) HB_INLINE {
-        return *reinterpret_cast<const __attribute__((address_space(3))) half8*>((at_k ^ (32 * s)) + buf * kStage + 32 * kPitch * block);
-    };
-    auto read_v = [&](int db, int key, int buf) HB_INLINE {   // 4 keys from `key` (+ 4 h) on of channel 32 db + c
-        return __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                             reinterpret_cast<__attribute__((address_space(3))) short4v*>((at_v ^ (64 * db)) + buf * kStage + key * kPitch)));
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i)
+        at_v[i] = lds0 + kMatrix + vrow * kPitch + ((16 * (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1))) ^ (16 * att_flip_v<PC>(vrow)) ^ (64 * i)) + 8 * (lane & 1);
+    auto read_k = [&](int step, int at) HB_INLINE { return *reinterpret_cast<const __attribute__((address_space(3))) half8*>(at_k[step] + at); };
+    auto read_v = [&](int block, int at) HB_INLINE {          // 4 keys from the one at `at` (+ 4 h) on of channel 32 block + c
+        return __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) short4v*>(at_v[block] + at)));
     };
 
     floatx16 o[kBlocks];
@@ -179,79 +191,119 @@ __global__ void __launch_bounds__(64 * kAttWaves, DP > 64 ? 2 : 3) attention_mfm
     float top = -INFINITY, base = 0.f, sum = 0.f;             // this row's largest score, or up to 8 less, and this lane's sum of weights
     bool far = false;                                         // scores beyond 2^13
 
+    auto attend = [&](uint64_t seen, auto index) HB_INLINE {
+        constexpr int kAt = decltype(index)::value * kStage;
+        floatx16 s[2];
+        {
+            half8 kf[2][kSteps];
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) kf[k][i] = read_k(i, kAt + 32 * kPitch * k);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[k][j] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) s[k] = mfma32x32x16(kf[k][i], qf[i], s[k]);
+        }
+        if (~seen) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint32_t bits = (uint32_t)(seen >> (32 * k)) >> (4 * h);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[k][j] = (bits >> (8 * (j / 4) + j % 4)) & 1 ? s[k][j] : -INFINITY;
+            }
+        }
+        half4 vf[2][kBlocks];                                 // of the first 16 keys: on their way while the weights are computed
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) {
+            vf[0][i] = read_v(i, kAt);
+            vf[1][i] = read_v(i, kAt + 8 * kPitch);
+        }
+        // a NaN makes the maximum one, and then moves nothing; its weight makes the row one
+        float most = __builtin_elementwise_maximum(s[0][0], s[1][0]);
+#pragma unroll
+        for (int j = 1; j < 16; ++j) most = __builtin_elementwise_maximum(most, __builtin_elementwise_maximum(s[0][j], s[1][j]));
+        {
+            const uint32_t bits = __builtin_bit_cast(uint32_t, most);
+            const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);         // of lanes c, and of lanes c + 32
+            const uint32_t low = both[0], high = both[1];
+            most = __builtin_elementwise_maximum(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)) * p.scale2;
+        }
+        // Weights are 2^7 at the maximum that they refer to: fp16 then holds those down to 2^-21 of it in full, and up to 2^8 more is
+        // as good, so that the sums are moved only where the maximum grows by more than that.
+        if (__any(most > top + 8.f)) {
+            const float before = top;
+            top = fmaxf(top, most);
+            base = top == -INFINITY ? 0.f : top - 7.f;
+            const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(before - top);
+            sum *= keep;
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[i][j] *= keep;
+            far = __any(fabsf(base) > 8192.f);
+        }
+        half8 w[4];
+        if (!far) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) w[j / 8][j % 8] = (half_t)__builtin_amdgcn_exp2f(fmaf(s[j / 16][j % 16], p.scale2, -base));
+        } else {                                              // the rounding of a product that large would show: the same product for maximum and score
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                float x = s[j / 16][j % 16] * p.scale2;
+                asm volatile("" : "+v"(x));
+                w[j / 8][j % 8] = (half_t)__builtin_amdgcn_exp2f(x - base);
+            }
+        }
+        typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+        const half2v ones = {1, 1};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            half8 v[kBlocks];
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) v[i] = join(vf[0][i], vf[1][i]);
+            if (k < 3) {
+#pragma unroll
+                for (int i = 0; i < kBlocks; ++i) {
+                    vf[0][i] = read_v(i, kAt + (16 * k + 16) * kPitch);
+                    vf[1][i] = read_v(i, kAt + (16 * k + 24) * kPitch);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_fdot2(half2v{w[k][2 * j], w[k][2 * j + 1]}, ones, sum, false);
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) o[i] = mfma32x32x16(v[i], w[k], o[i]);
+        }
+    };
+
     uint64_t seen = 0;
-    uint32_t byte = 0;
+    uint32_t byte = 1;
     if (first < last) {
-        seen = seen_of(first, byte_of(first));
+        if (mask) byte = mask_of(first);
+        seen = seen_of(first, byte);
         request(first, seen, 0);
-        byte = byte_of(min(first + 1, last - 1));
+        if (mask) byte = mask_of(first + 1);
     }
-    for (int t = first; t < last; ++t) {
-        const int buf = (t - first) & 1;
+    int t = first;
+    auto turn = [&](auto index) HB_INLINE {
         const uint64_t next = t + 1 < last ? seen_of(t + 1, byte) : 0;
         tk_wait_loads<0>();
         lds_barrier();
         if (t + 1 < last) {
-            request(t + 1, next, buf ^ 1);
-            byte = byte_of(min(t + 2, last - 1));
+            request(t + 1, next, decltype(index)::value ^ 1);
+            if (mask) byte = mask_of(t + 2);
         }
-        if (active && seen) {
-            floatx16 s[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[k][j] = 0.f;
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) s[k] = mfma32x32x16(read_k(k, i, buf), qf[i], s[k]);
-            }
-            if (~seen) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t bits = (uint32_t)(seen >> (32 * k)) >> (4 * h);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) s[k][j] = (bits >> (8 * (j / 4) + j % 4)) & 1 ? s[k][j] : -INFINITY;
-                }
-            }
-            float most = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-            for (int j = 1; j < 16; ++j) most = fmaxf(most, fmaxf(s[0][j], s[1][j]));
-            most = fmaxf(most, __shfl_xor(most, 32)) * p.scale2;
-            // Weights are 2^7 at the maximum that they refer to: fp16 then holds those down to 2^-21 of it in full, and up to 2^8 more is
-            // as good, so that the sums are moved only where the maximum grows by more than that.
-            if (__any(most > top + 8.f)) {
-                const float before = top;
-                top = fmaxf(top, most);
-                base = top == -INFINITY ? 0.f : top - 7.f;
-                const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(before - top);
-                sum *= keep;
-#pragma unroll
-                for (int i = 0; i < kBlocks; ++i)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) o[i][j] *= keep;
-                far = __any(fabsf(base) > 8192.f);
-            }
-            half8 w[4];
-            if (!far) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) w[j / 8][j % 8] = (half_t)__builtin_amdgcn_exp2f(fmaf(s[j / 16][j % 16], p.scale2, -base));
-            } else {                                          // the rounding of a product that large would show: the same product for maximum and score
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    float x = s[j / 16][j % 16] * p.scale2;
-                    asm volatile("" : "+v"(x));
-                    w[j / 8][j % 8] = (half_t)__builtin_amdgcn_exp2f(x - base);
-                }
-            }
-            typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-            const half2v ones = {1, 1};
-#pragma unroll
-            for (int j = 0; j < 16; ++j) sum = __builtin_amdgcn_fdot2(half2v{w[j / 4][2 * (j % 4)], w[j / 4][2 * (j % 4) + 1]}, ones, sum, false);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int i = 0; i < kBlocks; ++i) o[i] = mfma32x32x16(join(read_v(i, 16 * k, buf), read_v(i, 16 * k + 8, buf)), w[k], o[i]);
-        }
+        if (active && seen) attend(seen, index);
         seen = next;
+        ++t;
+    };
+    while (t < last) {
+        turn(TkInt<0>{});
+        if (t < last) turn(TkInt<1>{});
     }
     sum += __shfl_xor(sum, 32);
     if (PARTS) {
