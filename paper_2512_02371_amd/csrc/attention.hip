@@ -97,7 +97,7 @@ __device__ __forceinline__ int att_flip_v(int row) { return PC == 8 ? (row << 1)
 
 // D rounded up to DP; PARTS: the sums go to the workspace.
 template <int DP, bool PARTS>
-__global__ void __launch_bounds__(64 * kAttWaves, DP > 64 ? 2 : 3) attention_mfma_kernel(AttentionArgs p) {
+__global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(AttentionArgs p) {
     constexpr int PC = DP <= 64 ? 8 : 16, kSteps = DP / 16, kBlocks = DP / 32;
     constexpr int kPitch = 16 * PC, kMatrix = 64 * kPitch, kStage = 2 * kMatrix;      // bytes: a row, a tile of k or v, both
     constexpr int kOwn = PC / 4, kRowsOf = 64 / PC;                                    // copies of 1 KB per matrix and wave, rows in one
@@ -188,8 +188,9 @@ __global__ void __launch_bounds__(64 * kAttWaves, DP > 64 ? 2 : 3) attention_mfm
     for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-    float top = -INFINITY, base = 0.f, sum = 0.f;             // this row's largest score, or up to 8 less, and this lane's sum of weights
-    bool far = false;                                         // scores beyond 2^13
+    float top = -INFINITY, base = 0.f;                        // the score that this row's weights refer to
+    float sums[4] = {0.f, 0.f, 0.f, 0.f};                     // of this lane's weights
+    bool careful = true;                                      // a row has no such score yet, or scores are beyond 2^13
 
     auto attend = [&](uint64_t seen, auto index) HB_INLINE {
         constexpr int kAt = decltype(index)::value * kStage;
@@ -217,50 +218,63 @@ __global__ void __launch_bounds__(64 * kAttWaves, DP > 64 ? 2 : 3) attention_mfm
                 for (int j = 0; j < 16; ++j) s[k][j] = (bits >> (8 * (j / 4) + j % 4)) & 1 ? s[k][j] : -INFINITY;
             }
         }
+        half8 w[4];
         half4 vf[2][kBlocks];                                 // of the first 16 keys: on their way while the weights are computed
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
             vf[0][i] = read_v(i, kAt);
             vf[1][i] = read_v(i, kAt + 8 * kPitch);
         }
-        // a NaN makes the maximum one, and then moves nothing; its weight makes the row one
-        float most = __builtin_elementwise_maximum(s[0][0], s[1][0]);
+        // Weights are 2^7 at the score that they refer to, the largest of a first tile: fp16 then holds those down to 2^-21 of it in full, and
+        // up to 2^8 more is as good.  So they are computed first; only where one is larger the maximum is sought and the sums are moved.
+        float part[4];
+        auto weigh = [&](auto power) HB_INLINE {
+            floatx16 e[2];
 #pragma unroll
-        for (int j = 1; j < 16; ++j) most = __builtin_elementwise_maximum(most, __builtin_elementwise_maximum(s[0][j], s[1][j]));
-        {
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) e[k][j] = power(s[k][j]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) part[j] = e[0][j];
+#pragma unroll
+            for (int j = 4; j < 32; ++j) part[j % 4] += e[j / 16][j % 16];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) w[j / 8][j % 8] = (half_t)e[j / 16][j % 16];
+        };
+        bool redo = careful;
+        if (!careful) {
+            weigh([&](float x) HB_INLINE { return __builtin_amdgcn_exp2f(fmaf(x, p.scale2, -base)); });
+            redo = __any((part[0] + part[1]) + (part[2] + part[3]) > 32768.f);
+        }
+        if (redo) {
+            // a NaN makes the maximum one, and then moves nothing; its weight makes the row one
+            float most = __builtin_elementwise_maximum(s[0][0], s[1][0]);
+#pragma unroll
+            for (int j = 1; j < 16; ++j) most = __builtin_elementwise_maximum(most, __builtin_elementwise_maximum(s[0][j], s[1][j]));
             const uint32_t bits = __builtin_bit_cast(uint32_t, most);
             const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);         // of lanes c, and of lanes c + 32
             const uint32_t low = both[0], high = both[1];
             most = __builtin_elementwise_maximum(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high)) * p.scale2;
-        }
-        // Weights are 2^7 at the maximum that they refer to: fp16 then holds those down to 2^-21 of it in full, and up to 2^8 more is
-        // as good, so that the sums are moved only where the maximum grows by more than that.
-        if (__any(most > top + 8.f)) {
             const float before = top;
             top = fmaxf(top, most);
             base = top == -INFINITY ? 0.f : top - 7.f;
             const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(before - top);
-            sum *= keep;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sums[j] *= keep;
 #pragma unroll
             for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) o[i][j] *= keep;
-            far = __any(fabsf(base) > 8192.f);
-        }
-        half8 w[4];
-        if (!far) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) w[j / 8][j % 8] = (half_t)__builtin_amdgcn_exp2f(fmaf(s[j / 16][j % 16], p.scale2, -base));
-        } else {                                              // the rounding of a product that large would show: the same product for maximum and score
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                float x = s[j / 16][j % 16] * p.scale2;
+            careful = __any(top == -INFINITY || fabsf(base) > 8192.f);
+            // the rounding of a large product would show: the same product for the maximum and for the scores
+            weigh([&](float x) HB_INLINE {
+                x *= p.scale2;
                 asm volatile("" : "+v"(x));
-                w[j / 8][j % 8] = (half_t)__builtin_amdgcn_exp2f(x - base);
-            }
+                return __builtin_amdgcn_exp2f(x - base);
+            });
         }
-        typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-        const half2v ones = {1, 1};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[j] += part[j];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             half8 v[kBlocks];
@@ -273,8 +287,6 @@ __global__ void __launch_bounds__(64 * kAttWaves, DP > 64 ? 2 : 3) attention_mfm
                     vf[1][i] = read_v(i, kAt + (16 * k + 24) * kPitch);
                 }
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum = __builtin_amdgcn_fdot2(half2v{w[k][2 * j], w[k][2 * j + 1]}, ones, sum, false);
 #pragma unroll
             for (int i = 0; i < kBlocks; ++i) o[i] = mfma32x32x16(v[i], w[k], o[i]);
         }
@@ -305,6 +317,7 @@ __global__ void __launch_bounds__(64 * kAttWaves, DP > 64 ? 2 : 3) attention_mfm
         turn(TkInt<0>{});
         if (t < last) turn(TkInt<1>{});
     }
+    float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     sum += __shfl_xor(sum, 32);
     if (PARTS) {
         if (active && row0 + c < rows) {

@@ -1,4 +1,6 @@
 // hb_rope_axes: rotary positions with several axes.
+#include <algorithm>
+
 #include "hb_device.hpp"
 #include "hb_host.hpp"
 
@@ -13,6 +15,7 @@ struct RopeArgs {
     int64_t x_batch, x_token, x_head, out_batch, out_token, out_head, pos_batch, pos_token;
     int end[HB_ROPE_MAX_AXES];     // the first pair beyond each axis' section
     int interleaved;
+    int groups;                    // threads that share the heads of a token and its pairs
 };
 
 // cos and sin of pos * freq radians.  The product is taken in turns, as a sum of two floats (Dekker: the fused multiply-add
@@ -44,29 +47,96 @@ __device__ __forceinline__ int rope_axis(const RopeArgs& p, int pair) {
     return a;
 }
 
-// A thread per pair (or channel beyond the pairs) of one token, all heads.
+// Bound by reading x and writing out once.  A thread turns V pairs of one token (8 that lie P channels apart, 16 bytes each, or 4 that lie
+// together, 16 bytes) in every kHeads-th head from its own on: the angles' cost is shared by the heads, and the loads of several heads are on
+// their way at the same time.  Threads beyond the pairs copy V pairs' worth of channels.  V = 1: any address.
+template <int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) rope_kernel(RopeArgs p) {
-    const int per = p.P + (p.D - 2 * p.P);
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t >= (int64_t)p.B * p.L * per) return;
-    const int e = (int)(t % per);
-    const int64_t tok = t / per;
-    const int l = (int)(tok % p.L), b = (int)(tok / p.L);
+    constexpr int W = INTERLEAVED ? 2 * V : V;            // channels in one access
+    typedef half_t vec __attribute__((ext_vector_type(W), aligned(V == 1 ? 2 : 2 * W)));
+    const int turning = p.P / V, rest = p.D - 2 * p.P, copied = (rest + W - 1) / W, per = turning + copied;
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, total = (int64_t)p.B * p.L * p.groups * per;
+    if (t >= total) return;
+    int e, group, l, b;
+    auto place = [&](auto at) {                           // of t, in 32 bits where these hold it: a division in 64 takes 100 instructions
+        using T = decltype(at);
+        const T u = at / (T)per, tok = u / (T)p.groups;
+        e = (int)(at - u * (T)per);
+        group = (int)(u - tok * (T)p.groups);
+        b = (int)(tok / (T)p.L);
+        l = (int)(tok - (T)b * (T)p.L);
+    };
+    if (total <= 0x7fffffff) place((uint32_t)t);
+    else place((uint64_t)t);
     const half_t* x = p.x + b * p.x_batch + l * p.x_token;
     half_t* o = p.out + b * p.out_batch + l * p.out_token;
-    if (e >= p.P) {
-        const int d = e + p.P;
-        for (int h = 0; h < p.H; ++h) o[h * p.out_head + d] = x[h * p.x_head + d];
+    constexpr int U = 4;                                  // heads at a time
+    if (e >= turning) {
+        const int d = 2 * p.P + (e - turning) * W;
+        for (int h = group; h < p.H; h += p.groups) {
+            const half_t* from = x + (int64_t)h * p.x_head + d;
+            half_t* to = o + (int64_t)h * p.out_head + d;
+            if (d + W <= p.D) *reinterpret_cast<vec*>(to) = *reinterpret_cast<const vec*>(from);
+            else *to = *from;                             // one channel behind the last pair
+        }
         return;
     }
-    float co, si;
-    rope_turn(p.pos[b * p.pos_batch + l * p.pos_token + rope_axis(p, e)], p.freq[e], co, si);
-    const int du = p.interleaved ? 2 * e : e, dv = p.interleaved ? 2 * e + 1 : e + p.P;
-    for (int h = 0; h < p.H; ++h) {
-        const float u = x[h * p.x_head + du], v = x[h * p.x_head + dv];
-        o[h * p.out_head + du] = (half_t)(u * co - v * si);
-        o[h * p.out_head + dv] = (half_t)(v * co + u * si);
+    float co[V], si[V];
+    const int32_t* pos = p.pos + b * p.pos_batch + l * p.pos_token;
+#pragma unroll
+    for (int i = 0; i < V; ++i) rope_turn(pos[rope_axis(p, e * V + i)], p.freq[e * V + i], co[i], si[i]);
+    const int d0 = e * W, d1 = INTERLEAVED ? d0 : d0 + p.P;
+    auto turn = [&](vec& a, vec& c) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float f = INTERLEAVED ? a[2 * i % W] : a[i % W], g = INTERLEAVED ? a[(2 * i + 1) % W] : c[i % W];
+            const half_t r = (half_t)(f * co[i] - g * si[i]), s = (half_t)(g * co[i] + f * si[i]);
+            if (INTERLEAVED) {
+                a[2 * i % W] = r;
+                a[(2 * i + 1) % W] = s;
+            } else {
+                a[i % W] = r;
+                c[i % W] = s;
+            }
+        }
+    };
+    int h = group;
+    for (; h + (U - 1) * p.groups < p.H; h += U * p.groups) {
+        vec a[U], c[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const half_t* q = x + (int64_t)(h + i * p.groups) * p.x_head;
+            a[i] = *reinterpret_cast<const vec*>(q + d0);
+            if (!INTERLEAVED) c[i] = *reinterpret_cast<const vec*>(q + d1);
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            turn(a[i], c[i]);
+            half_t* q = o + (int64_t)(h + i * p.groups) * p.out_head;
+            *reinterpret_cast<vec*>(q + d0) = a[i];
+            if (!INTERLEAVED) *reinterpret_cast<vec*>(q + d1) = c[i];
+        }
     }
+    for (; h < p.H; h += p.groups) {
+        vec a = *reinterpret_cast<const vec*>(x + (int64_t)h * p.x_head + d0), c = a;
+        if (!INTERLEAVED) c = *reinterpret_cast<const vec*>(x + (int64_t)h * p.x_head + d1);
+        turn(a, c);
+        *reinterpret_cast<vec*>(o + (int64_t)h * p.out_head + d0) = a;
+        if (!INTERLEAVED) *reinterpret_cast<vec*>(o + (int64_t)h * p.out_head + d1) = c;
+    }
+}
+
+template <int V, bool INTERLEAVED>
+static hb_status rope_launch(RopeArgs a, hipStream_t st) {
+    constexpr int W = INTERLEAVED ? 2 * V : V;
+    const int64_t per_token = a.P / V + (a.D - 2 * a.P + W - 1) / W;
+    // heads are shared out until there are about four waves a SIMD
+    const int64_t threads = a.B * (int64_t)a.L * per_token, wanted = (int64_t)num_cu() * 1024;
+    a.groups = (int)std::min<int64_t>(a.H, std::max<int64_t>(1, wanted / threads));
+    const int64_t blocks = (threads * a.groups + 255) / 256;
+    if (blocks > 0x7fffffff) return HB_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((rope_kernel<V, INTERLEAVED>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    return launch_status();
 }
 
 }  // namespace hb
@@ -81,7 +151,7 @@ extern "C" hb_status hb_rope_axes(const hb_half* x, hb_half* out, const int32_t*
         if (s < 0) return HB_ERR_INVALID_ARG;
     if (axes > HB_ROPE_MAX_AXES || D > 65536) return HB_ERR_UNSUPPORTED;
     RopeArgs a = {reinterpret_cast<const half_t*>(x), reinterpret_cast<half_t*>(out), positions, freq, B, L, H, D, 0,
-                  x_batch, x_token, x_head, out_batch, out_token, out_head, pos_batch, pos_token, {}, interleaved != 0};
+                  x_batch, x_token, x_head, out_batch, out_token, out_head, pos_batch, pos_token, {}, interleaved != 0, 1};
     int64_t pairs = 0;
     for (int i = 0; i < HB_ROPE_MAX_AXES; ++i) {
         if (i < axes && sections[i] < 0) return HB_ERR_INVALID_ARG;
@@ -91,8 +161,9 @@ extern "C" hb_status hb_rope_axes(const hb_half* x, hb_half* out, const int32_t*
     }
     if (pairs < 1) return HB_ERR_INVALID_ARG;
     a.P = (int)pairs;
-    const int64_t blocks = ((int64_t)B * L * (D - a.P) + 255) / 256;
-    if (blocks > 0x7fffffff) return HB_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(rope_kernel, dim3((unsigned)blocks), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
-    return launch_status();
+    const auto st = reinterpret_cast<hipStream_t>(stream);
+    const int64_t strides = x_batch | x_token | x_head | out_batch | out_token | out_head;
+    const bool aligned = aligned_to(x, 16) && aligned_to(out, 16) && strides % 8 == 0;
+    if (interleaved) return aligned && a.P % 4 == 0 && D % 8 == 0 ? rope_launch<4, true>(a, st) : rope_launch<1, true>(a, st);
+    return aligned && a.P % 8 == 0 && D % 8 == 0 ? rope_launch<8, false>(a, st) : rope_launch<1, false>(a, st);
 }
