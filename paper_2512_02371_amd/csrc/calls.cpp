@@ -22,7 +22,7 @@ PyObject* g_error = nullptr;                  // hb.HbError
 PyTypeObject* g_ndarray = nullptr;
 bool g_forked = false;                        // a child of fork() cannot use its parent's device: hb.py lets torch say so
 
-#define HB_CALLS(X) X(hb_fir1d) X(hb_conv2d) X(hb_down2) X(hb_up2) X(hb_sepblur) X(hb_sat2d) X(hb_conv3x3) X(hb_pyr_level) X(hb_resize) X(hb_iir2) X(hb_dct_denoise)
+#define HB_CALLS(X) X(hb_fir1d) X(hb_conv2d) X(hb_down2) X(hb_up2) X(hb_sepblur) X(hb_sat2d) X(hb_conv3x3) X(hb_pyr_level) X(hb_resize) X(hb_iir2) X(hb_dct_denoise) X(hb_linear) X(hb_rope_axes) X(hb_attention)
 struct Library {
 #define HB_POINTER(f) decltype(&::f) f = nullptr;
     HB_CALLS(HB_POINTER)
@@ -270,6 +270,128 @@ PyObject* dct_denoise(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// Scratch memory, or none.
+bool scratch(PyObject* o, void*& p, size_t& n) {
+    p = nullptr;
+    n = 0;
+    return o == Py_None || bytes(o, false, p, n);
+}
+
+bool activation(PyObject* o, hb_act& act) {
+    static const struct {
+        const char* name;
+        hb_act act;
+    } known[] = {{"none", HB_ACT_NONE}, {"relu", HB_ACT_RELU}, {"gelu", HB_ACT_GELU}, {"gelu_tanh", HB_ACT_GELU_TANH}, {"silu", HB_ACT_SILU}};
+    if (!PyUnicode_CheckExact(o)) return false;
+    for (const auto& k : known)
+        if (PyUnicode_CompareWithASCIIString(o, k.name) == 0) {
+            act = k.act;
+            return true;
+        }
+    return false;
+}
+
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<7>(n, [&]() -> PyObject* {
+        Image x, w, o, r{};
+        const at::Tensor *out = plain(a[2]), *b = nullptr;
+        if (!out || (out->scalar_type() != at::kHalf && out->scalar_type() != at::kFloat)) Py_RETURN_FALSE;
+        const at::ScalarType type = out->scalar_type();
+        void* ws;
+        size_t size;
+        hb_act act;
+        if (!image(a[0], at::kHalf, 2, x) || !image(a[1], at::kHalf, 2, w) || !image(a[2], type, 2, o) || x.w != w.w || o.h != x.h || o.w != w.h ||
+            !scratch(a[3], ws, size) || !activation(a[6], act)) Py_RETURN_FALSE;
+        if (a[4] != Py_None) {
+            b = plain(a[4]);
+            if (!b || b->scalar_type() != at::kHalf || b->dim() != 1 || b->size(0) != w.h || !b->is_contiguous()) Py_RETURN_FALSE;
+        }
+        if (a[5] != Py_None && (!image(a[5], type, 2, r) || r.h != o.h || r.w != o.w)) Py_RETURN_FALSE;
+        if (x.h == 1) x.pitch = x.w, o.pitch = r.pitch = o.w;                 // the pitch of a single row has no meaning, and torch gives any
+        if (w.h == 1) w.pitch = w.w;
+        const hb_half* bias = b ? static_cast<const hb_half*>(b->data_ptr()) : nullptr;
+        return made("hb_linear", [&](hb_stream st) {
+            return g_lib.hb_linear(h(x.p), h(w.p), bias, r.p, o.p, type == at::kFloat ? HB_F32 : HB_F16, act, x.h, w.h, x.w, x.pitch, w.pitch, r.pitch, o.pitch,
+                                   ws, size, st);
+        });
+    });
+}
+
+// B x L x H x D, the last axis dense.
+struct Heads {
+    void* p;
+    int n[4];
+    int64_t s[3];
+};
+bool heads(PyObject* o, Heads& r) {
+    const at::Tensor* t = plain(o);
+    if (!t || t->dim() != 4 || t->scalar_type() != at::kHalf) return false;
+    for (int i = 0; i < 4; ++i) {
+        if (t->size(i) > kMostInt) return false;
+        r.n[i] = (int)t->size(i);
+        if (i < 3) r.s[i] = t->stride(i);
+    }
+    r.p = t->data_ptr();
+    return t->stride(3) == 1;
+}
+bool same(const Heads& a, const Heads& b) { return !memcmp(a.n, b.n, sizeof a.n); }
+
+PyObject* rope_axes(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<6>(n, [&]() -> PyObject* {
+        Heads x, o;
+        const at::Tensor *pos = plain(a[2]), *freq = plain(a[3]);
+        if (!heads(a[0], x) || !heads(a[1], o) || !same(x, o) || !pos || !freq || (!PyList_CheckExact(a[4]) && !PyTuple_CheckExact(a[4])) || !PyBool_Check(a[5])) Py_RETURN_FALSE;
+        const Py_ssize_t axes = PySequence_Fast_GET_SIZE(a[4]);
+        int32_t sections[HB_ROPE_MAX_AXES];
+        int64_t pairs = 0;
+        if (axes < 1 || axes > HB_ROPE_MAX_AXES) Py_RETURN_FALSE;
+        for (Py_ssize_t i = 0; i < axes; ++i) {
+            int v;
+            if (!integer(PySequence_Fast_GET_ITEM(a[4], i), v)) Py_RETURN_FALSE;
+            sections[i] = v;
+            pairs += v;
+        }
+        if (pos->scalar_type() != at::kInt || pos->dim() != 3 || pos->size(0) != x.n[0] || pos->size(1) != x.n[1] || pos->size(2) != axes || pos->stride(2) != 1 ||
+            freq->scalar_type() != at::kFloat || freq->dim() != 1 || freq->size(0) != pairs || !freq->is_contiguous()) Py_RETURN_FALSE;
+        const int32_t* pp = static_cast<const int32_t*>(pos->data_ptr());
+        const float* pf = static_cast<const float*>(freq->data_ptr());
+        const int64_t pb = pos->stride(0), pl = pos->stride(1);
+        const int together = a[5] == Py_True;
+        return made("hb_rope_axes", [&](hb_stream st) {
+            return g_lib.hb_rope_axes(h(x.p), h(o.p), pp, pf, x.n[0], x.n[1], x.n[2], x.n[3], x.s[0], x.s[1], x.s[2], o.s[0], o.s[1], o.s[2], pb, pl, sections, (int)axes,
+                                      together, st);
+        });
+    });
+}
+
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<8>(n, [&]() -> PyObject* {
+        Heads q, k, v, o;
+        float scale;
+        void* ws;
+        size_t size;
+        const at::Tensor *len = nullptr, *mask = nullptr;
+        if (!heads(a[0], q) || !heads(a[1], k) || !heads(a[2], v) || !heads(a[3], o) || !same(k, v) || !same(q, o) || q.n[0] != k.n[0] || q.n[3] != k.n[3] ||
+            !real(a[4], scale) || !scratch(a[5], ws, size)) Py_RETURN_FALSE;
+        if (a[6] != Py_None) {
+            len = plain(a[6]);
+            if (!len || len->scalar_type() != at::kInt || len->dim() != 1 || len->size(0) != q.n[0] || !len->is_contiguous()) Py_RETURN_FALSE;
+        }
+        if (a[7] != Py_None) {
+            mask = plain(a[7]);
+            if (!mask || (mask->scalar_type() != at::kByte && mask->scalar_type() != at::kBool) || mask->dim() != 2 || mask->size(0) != k.n[0] || mask->size(1) != k.n[1] ||
+                mask->stride(1) != 1) Py_RETURN_FALSE;
+        }
+        const int32_t* pl = len ? static_cast<const int32_t*>(len->data_ptr()) : nullptr;
+        const uint8_t* pm = mask ? static_cast<const uint8_t*>(mask->data_ptr()) : nullptr;
+        const int64_t mp = mask ? mask->stride(0) : 0;
+        return made("hb_attention", [&](hb_stream st) {
+            return g_lib.hb_attention(h(q.p), h(k.p), h(v.p), h(o.p), q.n[0], q.n[1], k.n[1], q.n[2], k.n[2], q.n[3], q.s[0], q.s[1], q.s[2], k.s[0], k.s[1], k.s[2], v.s[0],
+                                      v.s[1], v.s[2], o.s[0], o.s[1], o.s[2], scale, pl, pm, mp, ws, size, st);
+        });
+    });
+}
+
 // bind({entry point: address}, error class): what load() found.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 2 || !PyDict_Check(a[0])) {
@@ -297,7 +419,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define HB_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HB_METHOD(bind), HB_METHOD(fir1d), HB_METHOD(conv2d), HB_METHOD(down2), HB_METHOD(up2), HB_METHOD(sepblur), HB_METHOD(sat2d),
-                         HB_METHOD(conv3x3), HB_METHOD(pyr_level), HB_METHOD(resize), HB_METHOD(iir2), HB_METHOD(dct_denoise), {nullptr, nullptr, 0, nullptr}};
+                         HB_METHOD(conv3x3), HB_METHOD(pyr_level), HB_METHOD(resize), HB_METHOD(iir2), HB_METHOD(dct_denoise), HB_METHOD(linear),
+                         HB_METHOD(rope_axes), HB_METHOD(attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -113,8 +113,8 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs p) {
         for (int i = 0; i < U; ++i) {
             turn(a[i], c[i]);
             half_t* q = o + (int64_t)(h + i * p.groups) * p.out_head;
-            *reinterpret_cast<vec*>(q + d0) = a[i];
-            if (!INTERLEAVED) *reinterpret_cast<vec*>(q + d1) = c[i];
+            __builtin_nontemporal_store(a[i], reinterpret_cast<vec*>(q + d0));
+            if (!INTERLEAVED) __builtin_nontemporal_store(c[i], reinterpret_cast<vec*>(q + d1));
         }
     }
     for (; h < p.H; h += p.groups) {
@@ -130,8 +130,8 @@ template <int V, bool INTERLEAVED>
 static hb_status rope_launch(RopeArgs a, hipStream_t st) {
     constexpr int W = INTERLEAVED ? 2 * V : V;
     const int64_t per_token = a.P / V + (a.D - 2 * a.P + W - 1) / W;
-    // heads are shared out until there are about four waves a SIMD
-    const int64_t threads = a.B * (int64_t)a.L * per_token, wanted = (int64_t)num_cu() * 1024;
+    // heads are shared out until there are 16 waves a SIMD to come and go (4: 64 us for 24960 tokens, 24 heads of 128, 57 with 16)
+    const int64_t threads = a.B * (int64_t)a.L * per_token, wanted = (int64_t)num_cu() * 4096;
     a.groups = (int)std::min<int64_t>(a.H, std::max<int64_t>(1, wanted / threads));
     const int64_t blocks = (threads * a.groups + 255) / 256;
     if (blocks > 0x7fffffff) return HB_ERR_UNSUPPORTED;

@@ -510,6 +510,8 @@ def _linear(name, x, w, out, workspace, bias, residual, act):
 
 def hb_linear(x, w, out, workspace=None, bias=None, residual=None, act="none"):
     """out = act(x w^T + bias) + residual; x: M x K, w: N x K, out and residual: M x N, fp16 or fp32."""
+    if _calls is not None and _calls.linear(x, w, out, workspace, bias, residual, act):
+        return out
     return _linear("hb_linear", x, w, out, workspace, bias, residual, act)
 
 
@@ -526,6 +528,8 @@ def _heads(t):
 
 def hb_rope_axes(x, out, positions, freq, sections, interleaved=False):
     """Turns channel pairs of x (B x L x H x D) by positions (B x L x axes) times freq; out may be x."""
+    if _calls is not None and _calls.rope_axes(x, out, positions, freq, sections, interleaved):
+        return out
     px, (B, L, H, D), xs = _heads(x)
     po, shape, os_ = _heads(out)
     assert shape == x.shape, "output shape"
@@ -565,6 +569,8 @@ def _attention(name, q, k, v, out, scale, workspace, key_len, key_mask):
 
 def hb_attention(q, k, v, out, scale, workspace=None, key_len=None, key_mask=None):
     """out = softmax(scale q k^T) v over the visible keys; q, out: B x Lq x Hq x D, k, v: B x Lk x Hkv x D."""
+    if _calls is not None and _calls.attention(q, k, v, out, scale, workspace, key_len, key_mask):
+        return out
     return _attention("hb_attention", q, k, v, out, scale, workspace, key_len, key_mask)
 
 
