@@ -359,29 +359,44 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
     }
 }
 
-// The parts' sums of a row brought to their common maximum, in their order; a thread per four channels.
+// The parts' sums of a row brought to their common reference, in their order: a wave per row, first a lane per part (their weights), then a
+// lane per two channels.
 __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs p) {
-    const int per = p.D / 4, rows = p.Lq * p.group;
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, at = t / per, total = (int64_t)p.B * p.Hkv * rows;
+    const int lane = threadIdx.x & 63, rows = p.Lq * p.group;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), total = (int64_t)p.B * p.Hkv * rows;
     if (at >= total) return;
-    const int d = (int)(t - at * per) * 4;
-    const float *o = p.parts + at * p.D + d, *ml = p.parts + p.nparts * total * p.D + 2 * at;
-    float top = -INFINITY;
-    for (int s = 0; s < p.nparts; ++s) top = fmaxf(top, ml[2 * s * total]);
-    const float base = top == -INFINITY ? 0.f : top;
-    floatx4 v = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < p.nparts; ++s) {
-        const float w = __builtin_amdgcn_exp2f(ml[2 * s * total] - base);
-        sum += w * ml[2 * s * total + 1];
-        const floatx4 q = *reinterpret_cast<const floatx4*>(o + s * total * p.D);
+    typedef float floatx2 __attribute__((ext_vector_type(2)));
+    static_assert(kAttMostParts <= 64 && HB_ATTENTION_MAX_D <= 128);
+    const int d = min(2 * lane, p.D - 2);
+    const float* o = p.parts + at * p.D + d;
+    floatx2 ml = {-INFINITY, 0.f};
+    if (lane < p.nparts) ml = *reinterpret_cast<const floatx2*>(p.parts + p.nparts * total * p.D + 2 * (lane * total + at));
+    float top = ml[0];
+    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    const float w = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - top);      // a part that saw nothing has sums of 0, or NaN
+    float sum = w * ml[1];
+    for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m);
+    floatx2 v = {0.f, 0.f};
+    auto add = [&](const floatx2& q, int s) HB_INLINE {
+        const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s));
+        v[0] = fmaf(f, q[0], v[0]);
+        v[1] = fmaf(f, q[1], v[1]);
+    };
+    int s = 0;
+    for (; s + 8 <= p.nparts; s += 8) {
+        floatx2 q[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += w * q[i];
+        for (int i = 0; i < 8; ++i) q[i] = *reinterpret_cast<const floatx2*>(o + (s + i) * total * p.D);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) add(q[i], s + i);
     }
+    for (; s < p.nparts; ++s) add(*reinterpret_cast<const floatx2*>(o + s * total * p.D), s);
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     const int bh = (int)(at / rows), row = (int)(at - (int64_t)bh * rows), i = row / p.group, g = row - i * p.group, b = bh / p.Hkv, hk = bh - b * p.Hkv;
-    *reinterpret_cast<half4*>(p.out + b * p.out_batch + i * p.out_token + (hk * p.group + g) * p.out_head + d) = to_half4(v * inv);
+    if (2 * lane < p.D) {
+        typedef half_t half2v __attribute__((ext_vector_type(2)));
+        *reinterpret_cast<half2v*>(p.out + b * p.out_batch + i * p.out_token + (hk * p.group + g) * p.out_head + d) = half2v{(half_t)(v[0] * inv), (half_t)(v[1] * inv)};
+    }
 }
 
 static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_half* k, const hb_half* v, hb_half* out, int B, int Lq, int Lk,
@@ -449,10 +464,10 @@ extern "C" hb_status hb_attention(HB_ATTENTION_PARAMS) {
     const auto st = reinterpret_cast<hipStream_t>(stream);
     if (const size_t need = attention_workspace(B, Lq, Lk, Hq, Hkv, D)) {
         if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need) return HB_ERR_WORKSPACE;
-        a.nparts = attention_parts(B, Lq, Lk, Hq, Hkv);
+        a.nparts = attention_parts(B, Lq, Lk, Hq, Hkv, D);
         a.parts = static_cast<float*>(workspace);
         if (hb_status s = attention_run<true>(a, st)) return s;
-        const int64_t blocks = ((int64_t)B * Hq * Lq * (D / 4) + 255) / 256;
+        const int64_t blocks = ((int64_t)B * Hq * Lq + 3) / 4;
         hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
         return launch_status();
     }
