@@ -120,20 +120,6 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
     const int first = (int)((int64_t)all * part / p.nparts), last = (int)((int64_t)all * (part + 1) / p.nparts);
     const uint8_t* const mask = p.key_mask ? p.key_mask + b * p.mask_pitch : nullptr;
 
-    // queries: qf[s] lane (c, h) = channels 16 s + 8 h .. + 7 of row c
-    half8 qf[kSteps];
-    {
-        const int row = min(row0 + c, rows - 1), i = row / p.group, g = row - i * p.group;
-        const half_t* q = p.q + b * p.q_batch + i * p.q_token + (hk * p.group + g) * p.q_head + 8 * h;
-        const uint32_t turn = p.negate ? 0x80008000u : 0u;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            u32x4 v = {0, 0, 0, 0};
-            if (16 * s + 8 * h < p.D) v = *reinterpret_cast<const u32x4*>(q + 16 * s);
-            qf[s] = __builtin_bit_cast(half8, v ^ turn);
-        }
-    }
-
     // copies of a tile: slot `lane` of copy i is row kRowsOf * i + lane / PC, place lane % PC
     const char* const k0 = reinterpret_cast<const char*>(p.k + b * p.k_batch + hk * p.k_head);
     const char* const v0 = reinterpret_cast<const char*>(p.v + b * p.v_batch + hk * p.v_head);
@@ -192,6 +178,7 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
     float sums[4] = {0.f, 0.f, 0.f, 0.f};                     // of this lane's weights
     bool careful = true;                                      // a row has no such score yet, or scores are beyond 2^13
 
+    half8 qf[kSteps];                                         // queries: lane (c, h) has channels 16 s + 8 h .. + 7 of row c
     auto attend = [&](uint64_t seen, auto index) HB_INLINE {
         constexpr int kAt = decltype(index)::value * kStage;
         floatx16 s[2];
@@ -299,6 +286,18 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
         seen = seen_of(first, byte);
         request(first, seen, 0);
         if (mask) byte = mask_of(first + 1);
+    }
+    // behind the first tile's request: the queries are on their way with it
+    {
+        const int row = min(row0 + c, rows - 1), i = row / p.group, g = row - i * p.group;
+        const half_t* q = p.q + b * p.q_batch + i * p.q_token + (hk * p.group + g) * p.q_head + 8 * h;
+        const uint32_t turn = p.negate ? 0x80008000u : 0u;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            u32x4 v = {0, 0, 0, 0};
+            if (16 * s + 8 * h < p.D) v = *reinterpret_cast<const u32x4*>(q + 16 * s);
+            qf[s] = __builtin_bit_cast(half8, v ^ turn);
+        }
     }
     int t = first;
     auto turn = [&](auto index) HB_INLINE {

@@ -19,13 +19,24 @@ struct LinearArgs {
     int steps;                 // tiles: steps of 64 k of one part of the sum (blockIdx.y); the parts' results are out_pitch * M apart
 };
 
+// 1 / (1 + exp(-v)); the hardware's reciprocal is within 1 ulp, a division would take ten instructions.
+__device__ __forceinline__ float lin_sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * v)); }
 __device__ __forceinline__ float linear_act(float v, int act) {
     switch (act) {
         case HB_ACT_RELU: return v < 0.f ? 0.f : v;                       // a NaN stays one
-        case HB_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678f));
-        // (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
-        case HB_ACT_GELU_TANH: return v / (1.f + __expf(-1.5957691f * (v + 0.044715f * v * v * v)));
-        case HB_ACT_SILU: return v / (1.f + __expf(-v));
+        case HB_ACT_GELU: {
+            // v times the normal distribution at v, whose tail is exp(-v^2 / 2) times a polynomial in 1 / (1 + 0.3275911 |v| / sqrt 2): Abramowitz and
+            // Stegun, 7.1.26, half of the 1.5e-7 of its error function.  Without the difference 1 - erf, small results keep their digits.
+            const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, fabsf(v), 1.f));
+            const float q = 0.5f * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+            const float tail = q * __builtin_amdgcn_exp2f(-0.72134752f * v * v);
+            return v * (v < 0.f ? tail : 1.f - tail);
+        }
+        case HB_ACT_GELU_TANH: {                                              // (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
+            const float e = __builtin_amdgcn_exp2f(v * fmaf(v * v, -2.3022082f * 0.044715f, -2.3022082f));
+            return v * __builtin_amdgcn_rcpf(1.f + e);
+        }
+        case HB_ACT_SILU: return v * lin_sigmoid(v);
         default: return v;
     }
 }
@@ -100,7 +111,8 @@ __device__ __forceinline__ half8 lin_last8(const half_t* row, int k, int K) {
     return r;
 }
 
-// `count` of V adjacent elements, at any address that their type allows.
+// `count` of V adjacent elements, at any address that their type allows.  Stores are streaming: whole lines of a row leave at a time (8192 x 8192, K
+// 2048: 236 -> 228 us; 100000 x 200 fp32, K 96: 62 -> 43).
 template <int V, class T>
 __device__ __forceinline__ void lin_load(float (&v)[V], const T* from, int count) {
     typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
@@ -120,24 +132,33 @@ __device__ __forceinline__ void lin_store(T* to, const float (&v)[V], int count)
         vec q;
 #pragma unroll
         for (int i = 0; i < V; ++i) q[i] = (T)v[i];
-        *reinterpret_cast<vec*>(to) = q;
+        __builtin_nontemporal_store(q, reinterpret_cast<vec*>(to));
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i < count) to[i] = (T)v[i];
     }
 }
+// One branch for all of them: a branch for each would leave its exponential's latency bare.
 template <int V>
 __device__ __forceinline__ void lin_act(float (&v)[V], int act) {
-    if (act == HB_ACT_NONE) return;
+    auto all = [&](auto f) HB_INLINE {
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = linear_act(v[i], act);
+        for (int i = 0; i < V; ++i) v[i] = f(v[i]);
+    };
+    switch (act) {
+        case HB_ACT_RELU: return all([](float x) HB_INLINE { return linear_act(x, HB_ACT_RELU); });
+        case HB_ACT_GELU: return all([](float x) HB_INLINE { return linear_act(x, HB_ACT_GELU); });
+        case HB_ACT_GELU_TANH: return all([](float x) HB_INLINE { return linear_act(x, HB_ACT_GELU_TANH); });
+        case HB_ACT_SILU: return all([](float x) HB_INLINE { return linear_act(x, HB_ACT_SILU); });
+        default: return;
+    }
 }
 
 // The epilogue of a wave: its WM x WN sums leave through a patch of LDS that is its own (TILES x 16 rows of WN floats at a time), because a
 // lane holds four columns of one row of a fragment and 16 lanes 16 different rows: from the patch, whole runs of a row are
 // finished and stored, 16 bytes a lane.  The 16-byte pieces of a row stand at piece ^ row % 16 (writes meet no bank twice).
-template <class O, int WM, int WN, int TILES>
+template <class O, int WM, int WN, int TILES, int BATCH>
 __device__ __forceinline__ void lin_finish(const LinearArgs& p, O* out, const floatx4 (&acc)[WN / 16][WM / 16], float* patch, int m0, int n0) {
     static_assert(WN >= 32 && (WM / 16) % TILES == 0);
     constexpr int kFlip = WN / 4 < 16 ? WN / 4 - 1 : 15;
@@ -159,7 +180,7 @@ __device__ __forceinline__ void lin_finish(const LinearArgs& p, O* out, const fl
             }
         });
         wave_lds_fence();
-        constexpr int kPasses = 16 * TILES / kStep, kBatch = kPasses < 4 ? kPasses : 4;
+        constexpr int kPasses = 16 * TILES / kStep, kBatch = kPasses < BATCH ? kPasses : BATCH;
 #pragma unroll 1
         for (int q = 0; q < kPasses; q += kBatch) {
             float v[kBatch][V], res[kBatch][V];
@@ -180,11 +201,11 @@ __device__ __forceinline__ void lin_finish(const LinearArgs& p, O* out, const fl
                     for (int i = 0; i < 4; ++i) v[b][e + i] = t[i] + bias[e + i];
                 }
             }
+            lin_act<kBatch * V>(reinterpret_cast<float(&)[kBatch * V]>(v), p.act);
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 const int64_t m = m0 + 16 * h + (q + b) * kStep + r0;
                 if (m < p.M && count > 0) {
-                    lin_act<V>(v[b], p.act);
                     if (p.residual) {
 #pragma unroll
                         for (int i = 0; i < V; ++i) v[b][i] += res[b][i];
@@ -196,8 +217,7 @@ __device__ __forceinline__ void lin_finish(const LinearArgs& p, O* out, const fl
         wave_lds_fence();
     }
 }
-// Fragments of 16 rows in a wave's patch.
-constexpr int lin_patch_tiles(int WM) { return WM / 16 > 2 ? WM / 32 : WM / 16; }
+constexpr int kLinPatch = 1;                              // fragments of 16 rows in a patch
 
 // Which tile a workgroup takes: groups of 8 tile rows, column after column, in the order in which the workgroups of one XCD follow
 // each other, so that what runs there at one time shares rows and columns in its L2.
@@ -323,8 +343,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
         }
     }
     lds_barrier();
-    constexpr int kTiles = lin_patch_tiles(WM);
-    lin_finish<O, WM, WN, kTiles>(p, static_cast<O*>(p.out) + (int64_t)blockIdx.y * p.M * p.out_pitch, acc, reinterpret_cast<float*>(s_tiles) + 16 * kTiles * WN * wv,
+    lin_finish<O, WM, WN, kLinPatch, 4>(p, static_cast<O*>(p.out) + (int64_t)blockIdx.y * p.M * p.out_pitch, acc, reinterpret_cast<float*>(s_tiles) + 16 * kLinPatch * WN * wv,
                                   m0 + wm, n0 + wn);
 }
 
@@ -449,7 +468,7 @@ __global__ void __launch_bounds__(256, 1) linear_large_kernel(LinearArgs p) {
         }
         int tm, tn;
         lin_tile(tile, tiles_m, tiles_n, tm, tn);
-        lin_finish<O, 128, 128, 1>(p, static_cast<O*>(p.out), acc, reinterpret_cast<float*>(s_tiles + 2 * kStage) + 2048 * wv, tm * BM + wm, tn * BN + wn);
+        lin_finish<O, 128, 128, kLinPatch, 4>(p, static_cast<O*>(p.out), acc, reinterpret_cast<float*>(s_tiles + 2 * kStage) + 2048 * wv, tm * BM + wm, tn * BN + wn);
     }
     tk_wait_loads<0>();                                   // nothing may arrive in LDS that is no longer this workgroup's
 }
@@ -561,8 +580,10 @@ static hb_status linear_launch(const LinearArgs& a, int parts, hipStream_t st) {
     const int64_t tiles = (int64_t)ceil_div(a.M, BM) * ceil_div(a.N, BN);
     if (tiles > 0x7fffffff) return HB_ERR_UNSUPPORTED;
     auto kernel = linear_mfma_kernel<O, BM, BN, WM, WN, ROWS>;
-    constexpr int kStages = (BM + BN) * 256, kPatches = 64 * lin_patch_tiles(WM) * WN * (BM / WM) * (BN / WN);
-    constexpr int kLds = kStages > kPatches ? kStages : kPatches;
+    // one step needs one stage, and twice as many workgroups are on a compute unit (1M x 64, K 64, residual: 101 -> 93 us)
+    const int kStages = (BM + BN) * (a.steps > 1 || ROWS == kLinCopied ? 256 : 128);
+    constexpr int kPatches = 64 * kLinPatch * WN * (BM / WM) * (BN / WN);
+    const int kLds = kStages > kPatches ? kStages : kPatches;
     if (kLds > 65536)
         if (hb_status s = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds)) return s;
     hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, parts), dim3(64 * (BM / WM) * (BN / WN)), kLds, st, a);
