@@ -167,6 +167,24 @@ __device__ __forceinline__ void lin_finish(const LinearArgs& p, O* out, const fl
     const int x = lane % kLanes * V, count = p.N - (n0 + x), r0 = lane / kLanes;
     float bias[V] = {};
     if (p.bias) lin_load<V>(bias, p.bias + n0 + x, count);
+    constexpr int kPasses = 16 * TILES / kStep, kBatch = kPasses < BATCH ? kPasses : BATCH;
+    // the residual of a batch of rows is requested while the batch before is finished
+    typedef O vec __attribute__((ext_vector_type(V), aligned(sizeof(O))));
+    vec ahead[kBatch] = {}, res[kBatch] = {};
+    auto request = [&](int first) HB_INLINE {
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int64_t m = m0 + first + b * kStep + r0;
+            const O* from = static_cast<const O*>(p.residual) + m * p.res_pitch + n0 + x;
+            if (m < p.M && first < WM) {
+                if (count >= V) ahead[b] = *reinterpret_cast<const vec*>(from);
+                else
+#pragma unroll
+                    for (int i = 0; i < V; ++i) ahead[b][i] = i < count ? from[i] : (O)0.f;
+            }
+        }
+    };
+    if (p.residual) request(0);
 #pragma unroll 1
     for (int h = 0; h < WM / 16; h += TILES) {
         tk_for<WM / 16>([&](auto tile) HB_INLINE {
@@ -180,17 +198,10 @@ __device__ __forceinline__ void lin_finish(const LinearArgs& p, O* out, const fl
             }
         });
         wave_lds_fence();
-        constexpr int kPasses = 16 * TILES / kStep, kBatch = kPasses < BATCH ? kPasses : BATCH;
 #pragma unroll 1
         for (int q = 0; q < kPasses; q += kBatch) {
-            float v[kBatch][V], res[kBatch][V];
-            if (p.residual) {
-#pragma unroll
-                for (int b = 0; b < kBatch; ++b) {
-                    const int64_t m = m0 + 16 * h + (q + b) * kStep + r0;
-                    if (m < p.M && count > 0) lin_load<V>(res[b], static_cast<const O*>(p.residual) + m * p.res_pitch + n0 + x, count);
-                }
-            }
+            float v[kBatch][V];
+            const int first = 16 * h + q * kStep;         // row of the wave
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
                 const int r = (q + b) * kStep + r0;
@@ -201,17 +212,22 @@ __device__ __forceinline__ void lin_finish(const LinearArgs& p, O* out, const fl
                     for (int i = 0; i < 4; ++i) v[b][e + i] = t[i] + bias[e + i];
                 }
             }
+            if (p.residual) {
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) res[b] = ahead[b];
+                request(first + kBatch * kStep);
+            }
             lin_act<kBatch * V>(reinterpret_cast<float(&)[kBatch * V]>(v), p.act);
+            if (p.residual) {
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[b][i] += (float)res[b][i];
+            }
 #pragma unroll
             for (int b = 0; b < kBatch; ++b) {
-                const int64_t m = m0 + 16 * h + (q + b) * kStep + r0;
-                if (m < p.M && count > 0) {
-                    if (p.residual) {
-#pragma unroll
-                        for (int i = 0; i < V; ++i) v[b][i] += res[b][i];
-                    }
-                    lin_store<V>(out + m * p.out_pitch + n0 + x, v[b], count);
-                }
+                const int64_t m = m0 + first + b * kStep + r0;
+                if (m < p.M && count > 0) lin_store<V>(out + m * p.out_pitch + n0 + x, v[b], count);
             }
         }
         wave_lds_fence();
@@ -598,7 +614,7 @@ static hb_status linear_run(const LinPlan& plan, LinRows rows, const LinearArgs&
         case kLinRows16: return odd ? linear_launch_rows<O, 1, 16, kLinOdd>(a, parts, st) : linear_launch_rows<O, 1, 16, kLinEven>(a, parts, st);
         case kLinRows32: return odd ? linear_launch_rows<O, 2, 8, kLinOdd>(a, parts, st) : linear_launch_rows<O, 2, 8, kLinEven>(a, parts, st);
         case kLinRows64: return odd ? linear_launch_rows<O, 4, 8, kLinOdd>(a, parts, st) : linear_launch_rows<O, 4, 8, kLinEven>(a, parts, st);
-        case kLinTile64: return odd ? linear_launch<O, 64, 64, 16, 64, kLinOdd>(a, parts, st) : linear_launch<O, 64, 64, 16, 64, kLinEven>(a, parts, st);
+        case kLinTile64: return odd ? linear_launch<O, 64, 64, 16, 32, kLinOdd>(a, parts, st) : linear_launch<O, 64, 64, 16, 32, kLinEven>(a, parts, st);
         case kLinTile128x64: return odd ? linear_launch<O, 128, 64, 32, 64, kLinOdd>(a, parts, st) : linear_launch<O, 128, 64, 32, 64, kLinEven>(a, parts, st);
         case kLinTile128: return rows == kLinCopied ? linear_launch<O, 128, 128, 64, 32, kLinCopied>(a, parts, st) : linear_launch<O, 128, 128, 64, 32, kLinOdd>(a, parts, st);
         default: return linear_launch_large<O>(a, st);

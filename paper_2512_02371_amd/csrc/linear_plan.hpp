@@ -19,24 +19,25 @@ struct LinPlan {
 // The time of a call in us, as a model with a few constants per kernel: a workgroup alone on a compute unit takes `alone` a step and
 // `begin` beside it, one of several `shared` and `end`; a kernel for few rows of x has its waves take turns at the steps.  `odd`:
 // what rows at odd addresses add.  The constants were fitted to 1200 calls of random sizes (1 .. 2^20 x 16 .. 8192, K 16 ..
-// 8192), each timed with every kernel and with 1 to 32 parts: the choice is on average 1.5 % behind the fastest.
+// 8192), each timed with every kernel and with 1 to 32 parts: the choice is on average 0.9 % behind the fastest.
 struct LinCost {
     int m, n;                     // outputs of a workgroup
     int waves;                    // that share the steps; 0: tiles
     double alone, shared, begin, end, odd;
 };
 constexpr LinCost kLinCost[kLinKernels] = {
-    {16, 16, 16, 0.350, 0.043, 0.21, 0.00, 0.12}, {32, 16, 8, 0.419, 0.070, 0.35, 0.00, 0.10}, {64, 16, 8, 0.582, 0.169, 0.27, 0.00, 0.11},
-    {64, 64, 0, 0.290, 0.192, 1.26, 0.90, 0.25},  {128, 64, 0, 1.328, 0.227, 1.00, 1.50, 0.27}, {128, 128, 0, 0.528, 0.393, 2.46, 1.34, 0.00},
-    {256, 256, 0, 0.497, 1.064, 3.00, 6.60, 0.00},
+    {16, 16, 16, 1.107, 0.110, 0.00, 0.00, 0.35}, {32, 16, 8, 0.721, 0.142, 0.64, 0.00, 0.60}, {64, 16, 8, 1.452, 0.257, 0.80, 0.00, 0.33},
+    {64, 64, 0, 0.303, 0.182, 1.55, 0.90, 1.02},  {128, 64, 0, 0.548, 0.370, 2.53, 1.58, 0.85}, {128, 128, 0, 0.557, 0.317, 1.91, 1.99, 0.00},
+    {256, 256, 0, 1.303, 1.230, 1.19, 8.62, 0.00},
 };
-constexpr double kLinLaunch = 3.3, kLinJoin = 1.2, kLinJoinPart = 0.05, kLinJoinRate = 12.5e6;      // us, us, us, bytes per us
+constexpr LinCost kLinCostTile128Held = {128, 128, 0, 0.794, 0.466, 3.17, 3.75, 0.37};             // through registers
+constexpr double kLinLaunch = 2.4, kLinJoin = 1.6, kLinJoinPart = 0.33, kLinJoinRate = 7.4e6;       // us, us, us, bytes per us
 
 inline double linear_cost(LinKernel kernel, int64_t M, int64_t N, int parts, int steps, LinRows rows) {
-    const LinCost& c = kLinCost[kernel];
+    const LinCost& c = kernel == kLinTile128 && rows != kLinCopied ? kLinCostTile128Held : kLinCost[kernel];
     const int64_t wgs = ((M + c.m - 1) / c.m) * ((N + c.n - 1) / c.n) * parts;
-    double slow = rows == kLinOdd ? 1.0 + c.odd : 1.0, t;
-    if (kernel == kLinTile128 && rows != kLinCopied) slow = 0.85;     // through registers: faster alone, and it waits for nobody
+    const double slow = rows == kLinOdd ? 1.0 + c.odd : 1.0;
+    double t;
     if (c.waves) {
         const double waves = (steps + c.waves - 1) / c.waves * c.alone, all = wgs / 256.0 * steps * c.shared;
         t = c.begin + (waves > all ? waves : all) * slow;
