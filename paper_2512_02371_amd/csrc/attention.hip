@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
     constexpr int kOutPitch = 2 * DP + 16;                                             // bytes of a row on its way out
     constexpr int kLds = 2 * kStage > kAttTile * kOutPitch ? 2 * kStage : kAttTile * kOutPitch;
     __shared__ __attribute__((aligned(1024))) char s_tiles[kLds];
+    __shared__ __attribute__((aligned(16))) float s_hidden[2][64];                     // of the tiles with hidden keys: 0, or -inf for these
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, h = lane >> 5;
 
@@ -147,6 +148,7 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
                 tk_dma16(rv, off_v[i], 0, to + 1024 * i + kMatrix);
             }
         } else {                                              // what is hidden arrives as zeros
+            if (wv == 0) s_hidden[buf][lane] = (seen >> lane) & 1 ? 0.f : -INFINITY;
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
                 const bool there = (seen >> (kRowsOf * (kOwn * wv + i) + lane / PC)) & 1;
@@ -182,28 +184,31 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
     auto attend = [&](uint64_t seen, auto index) HB_INLINE {
         constexpr int kAt = decltype(index)::value * kStage;
         floatx16 s[2];
-        {
+        auto score = [&]() HB_INLINE {
             half8 kf[2][kSteps];
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) kf[k][i] = read_k(i, kAt + 32 * kPitch * k);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[k][j] = 0.f;
-#pragma unroll
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) s[k] = mfma32x32x16(kf[k][i], qf[i], s[k]);
-        }
-        if (~seen) {
+        };
+        if (~seen) {                                          // the scores of hidden keys (whose k arrived as zeros) start from -inf
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t bits = (uint32_t)(seen >> (32 * k)) >> (4 * h);
+            for (int j = 0; j < 32; j += 4) {
+                const floatx4 e = *reinterpret_cast<const floatx4*>(&s_hidden[decltype(index)::value][2 * j + 4 * h]);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[k][j] = (bits >> (8 * (j / 4) + j % 4)) & 1 ? s[k][j] : -INFINITY;
+                for (int i = 0; i < 4; ++i) s[j / 16][j % 16 + i] = e[i];
             }
+            score();
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[k][j] = 0.f;
+            score();
         }
         half8 w[4];
         half4 vf[2][kBlocks];                                 // of the first 16 keys: on their way while the weights are computed
