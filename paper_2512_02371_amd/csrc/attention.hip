@@ -90,22 +90,28 @@ constexpr int kAttRows = 32, kAttWaves = 4, kAttTile = kAttRows * kAttWaves;
 
 // A tile of keys in LDS: rows of PC 16-byte pieces (8 up to 64 channels, else 16), a piece at place piece ^ flip: what the fragments' reads
 // take at one time (16 rows of one piece of k; 4 rows of 64 bytes of v) lies in different banks.
+template <int DP, int GROUPS>
+constexpr int kAttLds = GROUPS * (DP <= 64 ? 32768 : 65536);                           // two stages of a tile of k and v, for each group
 template <int PC>
 __device__ __forceinline__ int att_flip_k(int row) { return PC == 8 ? (row >> 1) & 7 : row & 15; }
 template <int PC>
 __device__ __forceinline__ int att_flip_v(int row) { return PC == 8 ? (row << 1) & 4 : (row << 2) & 12; }
 
-// D rounded up to DP; PARTS: the sums go to the workspace.
-template <int DP, bool PARTS>
-__global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(AttentionArgs p) {
+// D rounded up to DP; PARTS: the sums go to the workspace.  GROUPS 2: eight waves, four for the even tiles of the keys and four for the odd
+// ones, each with tiles of its own in LDS; they join their sums there.  A workgroup that has a compute unit to itself is done in half the time.
+template <int DP, int GROUPS, bool PARTS>
+__global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_kernel(AttentionArgs p) {
     constexpr int PC = DP <= 64 ? 8 : 16, kSteps = DP / 16, kBlocks = DP / 32;
     constexpr int kPitch = 16 * PC, kMatrix = 64 * kPitch, kStage = 2 * kMatrix;      // bytes: a row, a tile of k or v, both
     constexpr int kOwn = PC / 4, kRowsOf = 64 / PC;                                    // copies of 1 KB per matrix and wave, rows in one
     constexpr int kOutPitch = 2 * DP + 16;                                             // bytes of a row on its way out
-    constexpr int kLds = 2 * kStage > kAttTile * kOutPitch ? 2 * kStage : kAttTile * kOutPitch;
-    __shared__ __attribute__((aligned(1024))) char s_tiles[kLds];
-    __shared__ __attribute__((aligned(16))) float s_hidden[2][64];                     // of the tiles with hidden keys: 0, or -inf for these
-    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    static_assert(kAttLds<DP, GROUPS> >= GROUPS * 2 * kStage && kAttLds<DP, GROUPS> >= kAttTile * kOutPitch);
+    extern __shared__ __attribute__((aligned(1024))) char s_all[];
+    __shared__ __attribute__((aligned(16))) float s_hide[GROUPS][2][64];               // of the tiles with hidden keys: 0, or -inf for these
+    __shared__ float s_sums[GROUPS > 1 ? kAttWaves : 1][64][2];                        // references and sums of the second group's rows
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wv = wave % kAttWaves, team = wave / kAttWaves;
+    char* const s_tiles = s_all + team * 2 * kStage;
+    float(&s_hidden)[2][64] = s_hide[team];
     const int c = lane & 31, h = lane >> 5;
 
     // neighbouring workgroups read the same keys
@@ -286,11 +292,12 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
 
     uint64_t seen = 0;
     uint32_t byte = 1;
-    if (first < last) {
-        if (mask) byte = mask_of(first);
-        seen = seen_of(first, byte);
-        request(first, seen, 0);
-        if (mask) byte = mask_of(first + 1);
+    int t = first + team;
+    if (t < last) {
+        if (mask) byte = mask_of(t);
+        seen = seen_of(t, byte);
+        request(t, seen, 0);
+        if (mask) byte = mask_of(t + GROUPS);
     }
     // behind the first tile's request: the queries are on their way with it
     {
@@ -304,25 +311,49 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
             qf[s] = __builtin_bit_cast(half8, v ^ turn);
         }
     }
-    int t = first;
     auto turn = [&](auto index) HB_INLINE {
-        const uint64_t next = t + 1 < last ? seen_of(t + 1, byte) : 0;
+        const int then = t + GROUPS;
+        const uint64_t next = then < last ? seen_of(then, byte) : 0;
         tk_wait_loads<0>();
         lds_barrier();
-        if (t + 1 < last) {
-            request(t + 1, next, decltype(index)::value ^ 1);
-            if (mask) byte = mask_of(t + 2);
+        if (then < last) {
+            request(then, next, decltype(index)::value ^ 1);
+            if (mask) byte = mask_of(then + GROUPS);
         }
         if (active && seen) attend(seen, index);
         seen = next;
-        ++t;
+        t = then;
     };
-    while (t < last) {
+    for (int left = (last - first + GROUPS - 1) / GROUPS; left > 0; left -= 2) {          // as many turns for either group
         turn(TkInt<0>{});
-        if (t < last) turn(TkInt<1>{});
+        if (left > 1) turn(TkInt<1>{});
     }
     float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     sum += __shfl_xor(sum, 32);
+    if (GROUPS > 1) {
+        // the second group's sums, in the lanes' own order, through its tiles
+        lds_barrier();
+        float* const across = reinterpret_cast<float*>(s_all + 2 * kStage) + wv * (16 * kBlocks * 64) + lane;
+        if (team) {
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) across[(16 * i + j) * 64] = o[i][j];
+            s_sums[wv][lane][0] = top;
+            s_sums[wv][lane][1] = sum;
+        }
+        lds_barrier();
+        if (team) return;
+        const float other = s_sums[wv][lane][0], both = fmaxf(top, other);
+        // a group that saw nothing has sums of 0, or NaN
+        const float mine = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - both), theirs = other == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other - both);
+        sum = sum * mine + s_sums[wv][lane][1] * theirs;
+        top = both;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] = o[i][j] * mine + across[(16 * i + j) * 64] * theirs;
+    }
     if (PARTS) {
         if (active && row0 + c < rows) {
             const int64_t total = (int64_t)p.B * p.Hkv * rows, at = part * total + (int64_t)bh * rows + row0 + c;
@@ -340,10 +371,10 @@ __global__ void __launch_bounds__(64 * kAttWaves, 2) attention_mfma_kernel(Atten
         }
         return;
     }
-    // out: through LDS, whole rows
-    lds_barrier();
+    // out: through LDS, whole rows; in the tiles of the first group, which nobody reads any more
+    if (GROUPS == 1) lds_barrier();
     if (!active) return;
-    char* const patch = s_tiles + wv * kAttRows * kOutPitch;
+    char* const patch = s_all + wv * kAttRows * kOutPitch;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int i = 0; i < kBlocks; ++i)
@@ -423,16 +454,23 @@ static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_
     return HB_OK;
 }
 
-template <bool PARTS>
-static hb_status attention_run(const AttentionArgs& a, hipStream_t st) {
+template <int DP, int GROUPS, bool PARTS>
+static hb_status attention_launch(const AttentionArgs& a, hipStream_t st) {
     const int64_t wgs = (int64_t)a.B * a.Hkv * attention_tiles(a.Lq, a.group) * a.nparts;
     if (wgs > 0x7fffffff) return HB_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)wgs), block(64 * kAttWaves);
-    if (a.D <= 32) hipLaunchKernelGGL((attention_mfma_kernel<32, PARTS>), grid, block, 0, st, a);
-    else if (a.D <= 64) hipLaunchKernelGGL((attention_mfma_kernel<64, PARTS>), grid, block, 0, st, a);
-    else if (a.D <= 96) hipLaunchKernelGGL((attention_mfma_kernel<96, PARTS>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((attention_mfma_kernel<128, PARTS>), grid, block, 0, st, a);
+    const auto kernel = attention_mfma_kernel<DP, GROUPS, PARTS>;
+    constexpr int kLds = kAttLds<DP, GROUPS>;
+    if (kLds > 32768)
+        if (hb_status s = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds)) return s;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(64 * kAttWaves * GROUPS), kLds, st, a);
     return launch_status();
+}
+template <int GROUPS, bool PARTS>
+static hb_status attention_run(const AttentionArgs& a, hipStream_t st) {
+    if (a.D <= 32) return attention_launch<32, GROUPS, PARTS>(a, st);
+    if (a.D <= 64) return attention_launch<64, GROUPS, PARTS>(a, st);
+    if (a.D <= 96) return attention_launch<96, GROUPS, PARTS>(a, st);
+    return attention_launch<128, GROUPS, PARTS>(a, st);
 }
 
 }  // namespace hb
@@ -466,14 +504,13 @@ extern "C" hb_status hb_attention(HB_ATTENTION_PARAMS) {
     AttentionArgs a;
     if (hb_status s = HB_ATTENTION_PREPARE(a)) return s;
     const auto st = reinterpret_cast<hipStream_t>(stream);
-    if (const size_t need = attention_workspace(B, Lq, Lk, Hq, Hkv, D)) {
-        if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need) return HB_ERR_WORKSPACE;
-        a.nparts = attention_parts(B, Lq, Lk, Hq, Hkv, D);
-        a.parts = static_cast<float*>(workspace);
-        if (hb_status s = attention_run<true>(a, st)) return s;
-        const int64_t blocks = ((int64_t)B * Hq * Lq + 3) / 4;
-        hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
-        return launch_status();
-    }
-    return attention_run<false>(a, st);
+    const AttentionPlan plan = attention_plan(B, Lq, Lk, Hq, Hkv, D);
+    if (plan.parts == 1) return plan.groups > 1 ? attention_run<2, false>(a, st) : attention_run<1, false>(a, st);
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < attention_workspace(B, Lq, Lk, Hq, Hkv, D)) return HB_ERR_WORKSPACE;
+    a.nparts = plan.parts;
+    a.parts = static_cast<float*>(workspace);
+    if (hb_status s = plan.groups > 1 ? attention_run<2, true>(a, st) : attention_run<1, true>(a, st)) return s;
+    const int64_t blocks = ((int64_t)B * Hq * Lq + 3) / 4;
+    hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    return launch_status();
 }

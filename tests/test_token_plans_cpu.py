@@ -26,7 +26,7 @@ int main() {
         } else {
             int B, Lq, Lk, Hq, Hkv, D;
             if (scanf("%d %d %d %d %d %d", &B, &Lq, &Lk, &Hq, &Hkv, &D) != 6) return 1;
-            printf("%d %zu", attention_parts(B, Lq, Lk, Hq, Hkv, D), attention_workspace(B, Lq, Lk, Hq, Hkv, D));
+            printf("%d %zu", attention_plan(B, Lq, Lk, Hq, Hkv, D).parts, attention_workspace(B, Lq, Lk, Hq, Hkv, D));
         }
         printf("\n");
     }
