@@ -104,7 +104,8 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
     constexpr int PC = DP <= 64 ? 8 : 16, kSteps = DP / 16, kBlocks = DP / 32;
     constexpr int kPitch = 16 * PC, kMatrix = 64 * kPitch, kStage = 2 * kMatrix;      // bytes: a row, a tile of k or v, both
     constexpr int kOwn = PC / 4, kRowsOf = 64 / PC;                                    // copies of 1 KB per matrix and wave, rows in one
-    static_assert(kAttLds<DP, GROUPS> >= GROUPS * 2 * kStage);
+    constexpr int kOutPitch = 2 * DP + 16;                                             // bytes of a row on its way out
+    static_assert(kAttLds<DP, GROUPS> >= GROUPS * 2 * kStage && kAttLds<DP, GROUPS> >= kAttTile * kOutPitch);
     extern __shared__ __attribute__((aligned(1024))) char s_all[];
     __shared__ __attribute__((aligned(16))) float s_hide[GROUPS][2][64];               // of the tiles with hidden keys: 0, or -inf for these
     __shared__ float s_sums[GROUPS > 1 ? kAttWaves : 1][64][2];                        // references and sums of the second group's rows
@@ -370,24 +371,28 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
         }
         return;
     }
-    // out: lanes c and c + 32 hold channels 8 q .. + 3 and + 4 .. + 7 of a row; of two such q they exchange halves and store 16 bytes each
-    if (!active || row0 + c >= rows) return;
+    // out: through LDS, in the tiles of the first group, which nobody reads any more.  Whole rows past the caches: pieces of 32 bytes from
+    // registers took 46 us where this takes 42 (8 x 4096 queries, 77 keys, 16 heads of 64), and rows that the caches keep 46 too.
+    if (GROUPS == 1) lds_barrier();
+    if (!active) return;
+    char* const patch = s_all + wv * kAttRows * kOutPitch;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int row = row0 + c, i = row / p.group, g = row - i * p.group;
-    half_t* const to = p.out + b * p.out_batch + i * p.out_token + (hk * p.group + g) * p.out_head + 8 * h;
 #pragma unroll
-    for (int n = 0; n < kBlocks; ++n)
+    for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
-        for (int q = 0; q < 4; q += 2) {
-            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-            auto pack = [&](int j) HB_INLINE {
-                return __builtin_bit_cast(u32x2, to_half4(floatx4{o[n][4 * j], o[n][4 * j + 1], o[n][4 * j + 2], o[n][4 * j + 3]} * inv));
-            };
-            const u32x2 low = pack(q), high = pack(q + 1);
-            const auto e = __builtin_amdgcn_permlane32_swap(low[0], high[0], false, false), f = __builtin_amdgcn_permlane32_swap(low[1], high[1], false, false);
-            const u32x4 v = {e[0], f[0], e[1], f[1]};
-            if (32 * n + 8 * q + 8 * h < p.D) *reinterpret_cast<u32x4*>(to + 32 * n + 8 * q) = v;
-        }
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<half4*>(patch + c * kOutPitch + 2 * (32 * i + 8 * q + 4 * h)) =
+                to_half4(floatx4{o[i][4 * q], o[i][4 * q + 1], o[i][4 * q + 2], o[i][4 * q + 3]} * inv);
+    wave_lds_fence();
+    constexpr int kLanes = DP / 8 <= 8 ? 8 : 16;
+    const int piece = lane % kLanes;
+#pragma unroll
+    for (int r = lane / kLanes; r < kAttRows; r += 64 / kLanes) {
+        const int row = row0 + r, i = row / p.group, g = row - i * p.group;
+        if (row < rows && 8 * piece < p.D)
+            __builtin_nontemporal_store(*reinterpret_cast<const half8*>(patch + r * kOutPitch + 16 * piece),
+                                        reinterpret_cast<half8*>(p.out + b * p.out_batch + i * p.out_token + (hk * p.group + g) * p.out_head + 8 * piece));
+    }
 }
 
 // The parts' sums of a row brought to their common reference, in their order: a wave per row, first a lane per part (their weights), then a
