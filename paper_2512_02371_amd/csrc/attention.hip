@@ -97,6 +97,15 @@ __device__ __forceinline__ int att_flip_k(int row) { return PC == 8 ? (row >> 1)
 template <int PC>
 __device__ __forceinline__ int att_flip_v(int row) { return PC == 8 ? (row << 1) & 4 : (row << 2) & 12; }
 
+// A workgroup's place in the order of batch, key head, part and rows.  Without lengths every XCD takes a contiguous eighth.  With lengths
+// (`same` workgroups, a key head's, have one) that could give one XCD all the short batches: key heads go round the XCDs then, and those
+// that are left over when their number is no multiple of 8 are cut into eighths.  4 x 4096 queries, 16 heads of 64, 2048 to 4096 keys: 308
+// -> 247 us; all of 4096 keys: 322, and contiguous eighths 321; one query, 16384 keys, 4 x 8 heads over 32 of 128: 56 and 54.
+__device__ __forceinline__ int attention_place(int wg, int nwg, int same) {
+    const int first = same ? nwg / (8 * same) * (8 * same) : 0;
+    return wg < first ? xcd_blocked(wg, first, same) : first + xcd_contiguous(wg - first, nwg - first);
+}
+
 // D rounded up to DP; PARTS: the sums go to the workspace.  GROUPS 2: eight waves, four for the even tiles of the keys and four for the odd
 // ones, each with tiles of its own in LDS; they join their sums there.  A workgroup that has a compute unit to itself is done in half the time.
 template <int DP, int GROUPS, bool PARTS>
@@ -116,7 +125,7 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
 
     // neighbouring workgroups read the same keys
     const int rows = p.Lq * p.group, tiles = (rows + kAttTile - 1) / kAttTile;
-    const int id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int id = attention_place(blockIdx.x, gridDim.x, p.key_len ? tiles * p.nparts : 0);
     const int tile = id % tiles, part = id / tiles % p.nparts, bh = id / tiles / p.nparts;
     const int hk = bh % p.Hkv, b = bh / p.Hkv;
     const int row0 = tile * kAttTile + wv * kAttRows;
