@@ -245,8 +245,13 @@ __device__ __forceinline__ void lin_tile(int wg, int tiles_m, int tiles_n, int& 
 }
 
 // A workgroup of (BM / WM) x (BN / WN) waves computes BM x BN outputs, a wave WM x WN of them with v_mfma_f32_16x16x32_f16; the rows
-// of w are the product's rows, so that a lane ends with four adjacent n of one m.  Two stages of 64 k take turns in LDS.
-template <class O, int BM, int BN, int WM, int WN, LinRows ROWS>
+// of w are the product's rows, so that a lane ends with four adjacent n of one m.  Two stages of G steps of 64 k take turns in LDS.
+//
+// A lone workgroup of 64 x 64 is bound by the chain of a step (barrier, reads from LDS, products): two steps behind one barrier (1024 x 1024,
+// K 1024 8.3 -> 7.2 us; 1920 x 1088, K 1024 11.8 -> 9.9), and more stages without that gain nothing.  Of 128 x 128 two workgroups share a compute
+// unit instead.  Rows that are not copied pass through registers, where a second step gains nothing either (1917 x 1079, K 1023 18 us).
+// Few k are bound by memory (1M x 64, K 64 with residual: 80 us, 5.0 TB/s); odd rows by their loads, two or three for 16 bytes.
+template <class O, int BM, int BN, int WM, int WN, LinRows ROWS, int G>
 __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_kernel(LinearArgs p) {
     constexpr int kWaves = (BM / WM) * (BN / WN), kMT = WM / 16, kNT = WN / 16;
     constexpr int kPieces = (BM + BN) / 8, kOwn = kPieces / kWaves;          // copies of 1 KB (8 rows) per stage, and of a wave
@@ -283,14 +288,14 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
         off[i] = there ? (uint32_t)(at * (is_x ? p.x_pitch : p.w_pitch) * 2) + 16 * chunk_of(row) : kTkOutside;
     }
     const uint32_t lds0 = tk_lds_addr(s_tiles);
-    auto request = [&](int step) HB_INLINE {
+    auto request = [&](int step, int buf) HB_INLINE {
         const int k0 = step * kLinK;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
             uint32_t o = off[i];
-            if (step >= steps || (k0 + kLinK > K && k0 + 8 * chunk_of(row_of(i)) >= K)) o = kTkOutside;
+            if (k0 + kLinK > K && k0 + 8 * chunk_of(row_of(i)) >= K) o = kTkOutside;
             const bool is_x = 8 * (wv * kOwn + i) < BM;                      // uniform
-            tk_dma16(is_x ? rx : rw, o, (uint32_t)k0 * 2, lds0 + (step & 1) * kStage + 1024 * (wv * kOwn + i));
+            tk_dma16(is_x ? rx : rw, o, (uint32_t)k0 * 2, lds0 + buf * kStage + 1024 * (wv * kOwn + i));
         }
     };
     // or they pass through registers; rows beyond the matrix repeat its last one (their sums are dropped)
@@ -340,14 +345,21 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
         }
     };
     if (ROWS == kLinCopied) {
-        request(0);
-        for (int s = 0; s < steps; ++s) {
+        int buf = 0;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+            if (i == 0 || i < steps) request(i, i);
+        for (int s = 0; s < steps; s += G) {
             tk_wait_loads<0>();
             lds_barrier();
-            request(s + 1);                                                  // beyond the sum: zeros
-            compute(s & 1);
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (s + G + i < steps) request(s + G + i, G - buf + i);
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (i == 0 || s + i < steps) compute(buf + i);
+            buf = G - buf;
         }
-        tk_wait_loads<0>();                                                  // nothing may arrive in the patches below
     } else {
         fetch(0);
         put(0);
@@ -591,13 +603,13 @@ static hb_status linear_launch_large(const LinearArgs& a, hipStream_t st) {
     return launch_status();
 }
 
-template <class O, int BM, int BN, int WM, int WN, LinRows ROWS>
+template <class O, int BM, int BN, int WM, int WN, LinRows ROWS, int G>
 static hb_status linear_launch(const LinearArgs& a, int parts, hipStream_t st) {
     const int64_t tiles = (int64_t)ceil_div(a.M, BM) * ceil_div(a.N, BN);
     if (tiles > 0x7fffffff) return HB_ERR_UNSUPPORTED;
-    auto kernel = linear_mfma_kernel<O, BM, BN, WM, WN, ROWS>;
+    auto kernel = linear_mfma_kernel<O, BM, BN, WM, WN, ROWS, G>;
     // one step needs one stage, and twice as many workgroups are on a compute unit (1M x 64, K 64, residual: 101 -> 93 us)
-    const int kStages = (BM + BN) * (a.steps > 1 || ROWS == kLinCopied ? 256 : 128);
+    const int kStages = (BM + BN) * 128 * std::min(a.steps > G ? 2 * G : G, a.steps);
     constexpr int kPatches = 64 * kLinPatch * WN * (BM / WM) * (BN / WN);
     const int kLds = kStages > kPatches ? kStages : kPatches;
     if (kLds > 65536)
@@ -614,9 +626,12 @@ static hb_status linear_run(const LinPlan& plan, LinRows rows, const LinearArgs&
         case kLinRows16: return odd ? linear_launch_rows<O, 1, 16, kLinOdd>(a, parts, st) : linear_launch_rows<O, 1, 16, kLinEven>(a, parts, st);
         case kLinRows32: return odd ? linear_launch_rows<O, 2, 8, kLinOdd>(a, parts, st) : linear_launch_rows<O, 2, 8, kLinEven>(a, parts, st);
         case kLinRows64: return odd ? linear_launch_rows<O, 4, 8, kLinOdd>(a, parts, st) : linear_launch_rows<O, 4, 8, kLinEven>(a, parts, st);
-        case kLinTile64: return odd ? linear_launch<O, 64, 64, 16, 32, kLinOdd>(a, parts, st) : linear_launch<O, 64, 64, 16, 32, kLinEven>(a, parts, st);
-        case kLinTile128x64: return odd ? linear_launch<O, 128, 64, 32, 64, kLinOdd>(a, parts, st) : linear_launch<O, 128, 64, 32, 64, kLinEven>(a, parts, st);
-        case kLinTile128: return rows == kLinCopied ? linear_launch<O, 128, 128, 64, 32, kLinCopied>(a, parts, st) : linear_launch<O, 128, 128, 64, 32, kLinOdd>(a, parts, st);
+        case kLinTile64:
+            return rows == kLinCopied ? linear_launch<O, 64, 64, 16, 32, kLinCopied, 2>(a, parts, st)
+                   : odd              ? linear_launch<O, 64, 64, 16, 32, kLinOdd, 1>(a, parts, st)
+                                      : linear_launch<O, 64, 64, 16, 32, kLinEven, 1>(a, parts, st);
+        case kLinTile128x64: return odd ? linear_launch<O, 128, 64, 32, 64, kLinOdd, 1>(a, parts, st) : linear_launch<O, 128, 64, 32, 64, kLinEven, 1>(a, parts, st);
+        case kLinTile128: return rows == kLinCopied ? linear_launch<O, 128, 128, 64, 32, kLinCopied, 1>(a, parts, st) : linear_launch<O, 128, 128, 64, 32, kLinOdd, 1>(a, parts, st);
         default: return linear_launch_large<O>(a, st);
     }
 }

@@ -26,15 +26,19 @@ struct LinCost {
     double alone, shared, begin, end, odd;
 };
 constexpr LinCost kLinCost[kLinKernels] = {
-    {16, 16, 16, 1.107, 0.110, 0.00, 0.00, 0.35}, {32, 16, 8, 0.721, 0.142, 0.64, 0.00, 0.60}, {64, 16, 8, 1.452, 0.257, 0.80, 0.00, 0.33},
-    {64, 64, 0, 0.303, 0.182, 1.55, 0.90, 1.02},  {128, 64, 0, 0.548, 0.370, 2.53, 1.58, 0.85}, {128, 128, 0, 0.557, 0.317, 1.91, 1.99, 0.00},
-    {256, 256, 0, 1.303, 1.230, 1.19, 8.62, 0.00},
+    {16, 16, 16, 0.749, 0.068, 0.00, 0.00, 0.91}, {32, 16, 8, 0.953, 0.135, 0.00, 0.00, 0.70}, {64, 16, 8, 1.447, 0.264, 0.00, 0.00, 0.32},
+    {64, 64, 0, 0.353, 0.219, 1.29, 0.77, 0.62},  {128, 64, 0, 0.452, 0.358, 2.69, 1.55, 1.11}, {128, 128, 0, 0.528, 0.410, 1.63, 1.35, 0.00},
+    {256, 256, 0, 0.744, 1.149, 9.12, 9.24, 0.00},
 };
-constexpr LinCost kLinCostTile128Held = {128, 128, 0, 0.794, 0.466, 3.17, 3.75, 0.37};             // through registers
-constexpr double kLinLaunch = 2.4, kLinJoin = 1.6, kLinJoinPart = 0.33, kLinJoinRate = 7.4e6;       // us, us, us, bytes per us
+// 64 x 64 copied to LDS directly, 128 x 128 through registers; what one step alone, with half of the LDS, takes of 128 x 64.
+constexpr LinCost kLinCostTile64Copied = {64, 64, 0, 0.240, 0.184, 0.27, 0.60, 0.00}, kLinCostTile128Held = {128, 128, 0, 0.802, 0.296, 2.45, 2.90, 0.34};
+constexpr double kLinOneStep = 0.72;
+constexpr double kLinLaunch = 2.5, kLinJoin = 2.58, kLinJoinPart = 0.28, kLinJoinRate = 6.9e6;      // us, us, us, bytes per us
 
 inline double linear_cost(LinKernel kernel, int64_t M, int64_t N, int parts, int steps, LinRows rows) {
-    const LinCost& c = kernel == kLinTile128 && rows != kLinCopied ? kLinCostTile128Held : kLinCost[kernel];
+    const LinCost& c = kernel == kLinTile128 && rows != kLinCopied  ? kLinCostTile128Held
+                       : kernel == kLinTile64 && rows == kLinCopied ? kLinCostTile64Copied
+                                                                    : kLinCost[kernel];
     const int64_t wgs = ((M + c.m - 1) / c.m) * ((N + c.n - 1) / c.n) * parts;
     const double slow = rows == kLinOdd ? 1.0 + c.odd : 1.0;
     double t;
@@ -43,7 +47,7 @@ inline double linear_cost(LinKernel kernel, int64_t M, int64_t N, int parts, int
         t = c.begin + (waves > all ? waves : all) * slow;
     } else {
         const double one = steps * c.alone * slow + c.begin, all = (double)((wgs + 255) / 256) * (steps * c.shared * slow + c.end);
-        t = one > all ? one : all;
+        t = (one > all ? one : all) * (steps == 1 && kernel == kLinTile128x64 ? kLinOneStep : 1.0);
     }
     if (parts > 1) t += kLinJoin + parts * kLinJoinPart + 8.0 * parts * M * N / kLinJoinRate;
     return t + kLinLaunch;
