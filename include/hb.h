@@ -52,7 +52,7 @@
  *    None of it depends on the data of a call.
  *  - Every stage has a `_valu` twin with the same signature and results that uses
  *    only vector-ALU FMAs (no MFMA): the ablation that shows what the matrix units
- *    buy.
+ *    buy.  (hb_rope_axes, which has no product, has none.)
  */
 #ifndef HB_H
 #define HB_H
