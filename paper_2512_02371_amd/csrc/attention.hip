@@ -106,6 +106,11 @@ __device__ __forceinline__ int attention_place(int wg, int nwg, int same) {
     return wg < first ? xcd_blocked(wg, first, same) : first + xcd_contiguous(wg - first, nwg - first);
 }
 
+// What bounds it, by size (queries x keys, heads of 64 unless said): many keys, the power of matrix and vector units together (4 x 4096 x 4096, 16 heads
+// 310 us, 880 TFLOP/s at 1.8 GHz, 0.42 and 0.58 busy); few keys, a workgroup's chain from its queries to its rows, with two on a compute unit
+// (8 x 4096 x 77, 16 heads 37 us of 22 for the bytes); one query, memory (4 x 16384 keys, 8 heads of 128: 36 us, 4.7 TB/s, and the join).
+// Products of the next tile ahead of the weights gain 1 to 6 % with many keys and lose with few; a third stage of LDS gains nothing.
+//
 // D rounded up to DP; PARTS: the sums go to the workspace.  GROUPS 2: eight waves, four for the even tiles of the keys and four for the odd
 // ones, each with tiles of its own in LDS; they join their sums there.  A workgroup that has a compute unit to itself is done in half the time.
 template <int DP, int GROUPS, bool PARTS>
@@ -405,7 +410,7 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
 }
 
 // The parts' sums of a row brought to their common reference, in their order: a wave per row, first a lane per part (their weights), then a
-// lane per two channels.
+// lane per two channels.  Bound by its launch and two trips to memory (128 rows of 16 parts 4.2 us).
 __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs p) {
     const int lane = threadIdx.x & 63, rows = p.Lq * p.group;
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), total = (int64_t)p.B * p.Hkv * rows;

