@@ -249,7 +249,7 @@ __device__ __forceinline__ void lin_tile(int wg, int tiles_m, int tiles_n, int& 
 //
 // A lone workgroup of 64 x 64 is bound by the chain of a step (barrier, reads from LDS, products): two steps behind one barrier (1024 x 1024,
 // K 1024 8.3 -> 7.2 us; 1920 x 1088, K 1024 11.8 -> 9.9), and more stages without that gain nothing.  Of 128 x 128 two workgroups share a compute
-// unit instead.  Rows that are not copied pass through registers, where a second step gains nothing either (1917 x 1079, K 1023 18 us).
+// unit instead.  Rows that are not copied pass through registers (1917 x 1079, K 1023 16.4 us), where a second step gains nothing.
 // Few k are bound by memory (1M x 64, K 64 with residual: 80 us, 5.0 TB/s); odd rows by their loads, two or three for 16 bytes.
 template <class O, int BM, int BN, int WM, int WN, LinRows ROWS, int G>
 __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_kernel(LinearArgs p) {
@@ -299,32 +299,47 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
         }
     };
     // or they pass through registers; rows beyond the matrix repeat its last one (their sums are dropped)
-    half8 held[ROWS == kLinCopied ? 1 : kOwn];
-    const half_t* from[ROWS == kLinCopied ? 1 : kOwn];
+    constexpr int kHeld = ROWS == kLinCopied ? 1 : kOwn;
+    u32x4 held[kHeld];                                                       // as lin_get8 loads them, moved on their way to LDS
+    uint32_t next[kHeld];
+    const half_t* from[kHeld];
+    uint32_t odd[kHeld];
     if (ROWS != kLinCopied) {
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
             const int row = row_of(i);
             from[i] = row < BM ? x0 + min(row, p.M - 1 - m0) * p.x_pitch : w0 + min(row - BM, p.N - 1 - n0) * p.w_pitch;
             from[i] += 8 * chunk_of(row);
+            odd[i] = ROWS == kLinOdd ? (uint32_t)(uintptr_t)from[i] & 2u : 0u;
         }
     }
-    auto fetch = [&](int step) HB_INLINE {
-        const int k0 = step * kLinK;
-        if (k0 + kLinK <= K) {
+    auto fetch = [&](int step) HB_INLINE {                                   // 64 k that are all there
 #pragma unroll
-            for (int i = 0; i < kOwn; ++i) held[i] = lin_get8<ROWS>(from[i] + k0);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kOwn; ++i) {
-                const int k = k0 + 8 * chunk_of(row_of(i));
-                held[i] = lin_last8(from[i] + k0 - k, k, K);
-            }
+        for (int i = 0; i < kOwn; ++i) {
+            const char* at = reinterpret_cast<const char*>(from[i] + step * kLinK) - odd[i];
+            typedef u32x4 u32x4_u __attribute__((aligned(4)));
+            held[i] = *reinterpret_cast<const u32x4_u*>(at);
+            if (ROWS == kLinOdd) next[i] = *reinterpret_cast<const uint32_t*>(at + 8 * odd[i]);
         }
     };
-    auto put = [&](int buf) HB_INLINE {
+    auto fetch_last = [&](int step) HB_INLINE {                              // the rest of K, in place
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) *reinterpret_cast<half8*>(s_tiles + buf * kStage + 1024 * (wv * kOwn + i) + 16 * lane) = held[i];
+        for (int i = 0; i < kOwn; ++i) {
+            const int k = step * kLinK + 8 * chunk_of(row_of(i));
+            held[i] = __builtin_bit_cast(u32x4, lin_last8(from[i] + step * kLinK - k, k, K));
+        }
+    };
+    auto put = [&](int buf, auto moved) HB_INLINE {
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            u32x4 v = held[i];
+            if (ROWS == kLinOdd && decltype(moved)::value) {
+                const uint32_t shift = 8 * odd[i];
+                v = u32x4{__builtin_amdgcn_alignbit(v[1], v[0], shift), __builtin_amdgcn_alignbit(v[2], v[1], shift), __builtin_amdgcn_alignbit(v[3], v[2], shift),
+                          __builtin_amdgcn_alignbit(next[i], v[3], shift)};
+            }
+            *reinterpret_cast<u32x4*>(s_tiles + buf * kStage + 1024 * (wv * kOwn + i) + 16 * lane) = v;
+        }
     };
 
     const int wm = wv / (BN / WN) * WM, wn = wv % (BN / WN) * WN;
@@ -360,15 +375,50 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
                 if (i == 0 || s + i < steps) compute(buf + i);
             buf = G - buf;
         }
-    } else {
-        fetch(0);
-        put(0);
+    } else if (kOwn > 2) {
+        auto take = [&](int step) HB_INLINE {
+            if (step * kLinK + kLinK <= K) {
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) held[i] = __builtin_bit_cast(u32x4, lin_get8<ROWS>(from[i] + step * kLinK));
+            } else {
+                fetch_last(step);
+            }
+        };
+        take(0);
+        put(0, TkInt<0>{});
         for (int s = 0; s < steps; ++s) {
             lds_barrier();
-            if (s + 1 < steps) fetch(s + 1);
+            if (s + 1 < steps) take(s + 1);
             compute(s & 1);
-            if (s + 1 < steps) put((s + 1) & 1);
+            if (s + 1 < steps) put((s + 1) & 1, TkInt<0>{});
         }
+    } else {
+        // odd rows are moved behind the products, so that these need not wait for them (1917 x 1079, K 1023 19.2 -> 16.4 us; with more rows a wave, in
+        // the larger tiles, that is slower: 4000 x 4001, K 2001 119 -> 124)
+        const int whole = min(steps, K / kLinK);
+        if (whole > 0) {
+            fetch(0);
+            put(0, TkInt<1>{});
+        } else {
+            fetch_last(0);
+            put(0, TkInt<0>{});
+        }
+        int s = 0;
+        for (; s + 1 < whole; ++s) {
+            lds_barrier();
+            fetch(s + 1);
+            compute(s & 1);
+            put((s + 1) & 1, TkInt<1>{});
+        }
+        if (s + 1 < steps) {
+            lds_barrier();
+            fetch_last(s + 1);
+            compute(s & 1);
+            put((s + 1) & 1, TkInt<0>{});
+            ++s;
+        }
+        lds_barrier();
+        compute(s & 1);
     }
     lds_barrier();
     lin_finish<O, WM, WN, kLinPatch, 4>(p, static_cast<O*>(p.out) + (int64_t)blockIdx.y * p.M * p.out_pitch, acc, reinterpret_cast<float*>(s_tiles) + 16 * kLinPatch * WN * wv,

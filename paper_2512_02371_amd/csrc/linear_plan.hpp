@@ -27,7 +27,7 @@ struct LinCost {
 };
 constexpr LinCost kLinCost[kLinKernels] = {
     {16, 16, 16, 0.749, 0.068, 0.00, 0.00, 0.91}, {32, 16, 8, 0.953, 0.135, 0.00, 0.00, 0.70}, {64, 16, 8, 1.447, 0.264, 0.00, 0.00, 0.32},
-    {64, 64, 0, 0.353, 0.219, 1.29, 0.77, 0.62},  {128, 64, 0, 0.452, 0.358, 2.69, 1.55, 1.11}, {128, 128, 0, 0.528, 0.410, 1.63, 1.35, 0.00},
+    {64, 64, 0, 0.353, 0.219, 1.29, 0.77, 0.40},  {128, 64, 0, 0.452, 0.358, 2.69, 1.55, 1.11}, {128, 128, 0, 0.528, 0.410, 1.63, 1.35, 0.00},
     {256, 256, 0, 0.744, 1.149, 9.12, 9.24, 0.00},
 };
 // 64 x 64 copied to LDS directly, 128 x 128 through registers; what one step alone, with half of the LDS, takes of 128 x 64.
