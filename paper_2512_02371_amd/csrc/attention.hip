@@ -461,7 +461,7 @@ static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_
         if (s < 0 || s % 8 != 0) return HB_ERR_INVALID_ARG;
     if (key_mask && mask_pitch < 0) return HB_ERR_INVALID_ARG;
     if (D % 8 != 0 || D > HB_ATTENTION_MAX_D) return HB_ERR_UNSUPPORTED;
-    if (st[4] > (1 << 20) || st[7] > (1 << 20) || (int64_t)Lq * (Hq / Hkv) > 0x7fffff00) return HB_ERR_UNSUPPORTED;
+    if (st[4] > (1 << 20) || st[7] > (1 << 20) || (int64_t)Lq * (Hq / Hkv) > kAttMost || Lk > kAttMost) return HB_ERR_UNSUPPORTED;
     a = {reinterpret_cast<const half_t*>(q), reinterpret_cast<const half_t*>(k), reinterpret_cast<const half_t*>(v), reinterpret_cast<half_t*>(out),
          B, Lq, Lk, Hq, Hkv, D, Hq / Hkv, st[0], st[1], st[2], st[3], st[4], st[5], st[6], st[7], st[8], st[9], st[10], st[11],
          // a scale of 0 as one that is too small to tell: hidden scores are -inf, and that times 0 is no number
@@ -500,7 +500,7 @@ static hb_status attention_run(const AttentionArgs& a, hipStream_t st) {
                       out_batch, out_token, out_head}, scale, key_len, key_mask, mask_pitch)
 
 extern "C" size_t hb_attention_workspace_size(int B, int Lq, int Lk, int Hq, int Hkv, int D) {
-    if (B < 1 || Lq < 1 || Lk < 1 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv != 0 || (int64_t)Lq * (Hq / Hkv) > 0x7fffff00) return 0;
+    if (B < 1 || Lq < 1 || Lk < 1 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv != 0 || (int64_t)Lq * (Hq / Hkv) > hb::kAttMost || Lk > hb::kAttMost) return 0;
     return hb::attention_workspace(B, Lq, Lk, Hq, Hkv, D);
 }
 

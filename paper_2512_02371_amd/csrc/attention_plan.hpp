@@ -6,6 +6,8 @@
 namespace hb {
 
 constexpr int kAttMostParts = 64;
+// Most keys, and most rows of a key head: the kernels count both in 32 bits, and look up to three tiles of 64 keys past the last one.
+constexpr int kAttMost = 0x7fffff00;
 
 // Workgroups (128 rows each) per key head.
 inline int64_t attention_tiles(int Lq, int group) { return ((int64_t)Lq * group + 127) / 128; }
