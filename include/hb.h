@@ -392,9 +392,9 @@ hb_status hb_pyr_level_valu(const hb_half *in, float *residual, hb_half *down_or
  *     out[m][n] = act(sum_{k < K} x[m][k] w[n][k] + bias[n]) + residual[m][n]
  * x: M x K fp16, w: N x K fp16, bias: N fp16 or NULL, residual and out: M x N of out_type, residual may be NULL or `out`
  * itself with its pitch (in place).  The sum, the bias, the activation and the residual are fp32 and rounded once, to
- * out_type.  M, N, K >= 1; pitches in elements, >= the row, at most HB_LINEAR_MAX_PITCH (HB_ERR_UNSUPPORTED beyond; M times
- * a pitch may pass 2^32).  Base pointers need the alignment of their elements; fastest with 16-byte aligned pointers and
- * K and pitches that are multiples of 8.
+ * out_type.  M, N, K >= 1; pitches in elements, >= the row, at most HB_LINEAR_MAX_PITCH, M at most 2^31 - 256 (HB_ERR_UNSUPPORTED
+ * beyond; M times a pitch may pass 2^32).  Base pointers need the alignment of their elements; fastest with 16-byte aligned pointers
+ * and K and pitches that are multiples of 8.
  * `workspace`: device scratch of at least hb_linear_workspace_size(M, N, K) bytes, 256-byte aligned, contents undefined on
  * exit; concurrent calls need their own.  The size is 0, and the pointer may be NULL, where the sum over k is not split.
  */

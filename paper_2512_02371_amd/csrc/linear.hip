@@ -724,6 +724,7 @@ static hb_status linear_prepare(LinearArgs& a, const hb_half* x, const hb_half* 
     if (!aligned_to(x, 2) || !aligned_to(w, 2) || !aligned_to(bias, 2) || !aligned_to(residual, size) || !aligned_to(out, size)) return HB_ERR_INVALID_ARG;
     for (int64_t p : {x_pitch, w_pitch, res_pitch, out_pitch})
         if (p > HB_LINEAR_MAX_PITCH) return HB_ERR_UNSUPPORTED;
+    if (M > kLinMostRows) return HB_ERR_UNSUPPORTED;
     a = {reinterpret_cast<const half_t*>(x), reinterpret_cast<const half_t*>(w), reinterpret_cast<const half_t*>(bias), residual, out, M, N, K, act,
          x_pitch, w_pitch, res_pitch, out_pitch, (K - 1) / 64 + 1};
     return HB_OK;

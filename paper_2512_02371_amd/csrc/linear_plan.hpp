@@ -11,6 +11,9 @@ enum LinRows { kLinCopied, kLinEven, kLinOdd };
 
 enum LinKernel { kLinRows16, kLinRows32, kLinRows64, kLinTile64, kLinTile128x64, kLinTile128, kLinTile256, kLinKernels };
 
+// Most rows of x: the kernels number rows in 32 bits, up to the end of the last tile.
+constexpr int kLinMostRows = 0x7fffff00;
+
 struct LinPlan {
     LinKernel kernel;
     int parts, steps;             // of the sum, and steps of 64 k of one part

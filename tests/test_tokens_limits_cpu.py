@@ -31,3 +31,10 @@ def attention(lib, fn, B=1, Lq=1, Lk=1, Hq=1, Hkv=1, D=8, mask=None):
 def test_more_keys_than_tile_numbers_hold(lib, fn, Lk, mask):
     assert attention(lib, fn, Lk=Lk, mask=mask) == UNSUPPORTED
     assert lib.hb_attention_workspace_size(1, 1, Lk, 1, 1, 8) == 0
+
+
+@pytest.mark.parametrize("fn", ["hb_linear", "hb_linear_valu"])
+@pytest.mark.parametrize("M", [MOST + 1, (1 << 31) - 1])
+def test_linear_rows_within_a_tile_of_2_to_the_31(lib, fn, M):
+    for N, K in ((1, 1), (64, 64), (300, 300)):
+        assert getattr(lib, fn)(P, P, None, None, P, 0, 0, M, N, K, K, K, N, N, None, 0, None) == UNSUPPORTED
