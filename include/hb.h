@@ -393,8 +393,8 @@ hb_status hb_pyr_level_valu(const hb_half *in, float *residual, hb_half *down_or
  * x: M x K fp16, w: N x K fp16, bias: N fp16 or NULL, residual and out: M x N of out_type, residual may be NULL or `out`
  * itself with its pitch (in place).  The sum, the bias, the activation and the residual are fp32 and rounded once, to
  * out_type.  M, N, K >= 1; pitches in elements, >= the row, at most HB_LINEAR_MAX_PITCH, M at most 2^31 - 256 (HB_ERR_UNSUPPORTED
- * beyond; M times a pitch may pass 2^32).  Base pointers need the alignment of their elements; fastest with 16-byte aligned pointers
- * and K and pitches that are multiples of 8.
+ * beyond, and for the twin from 2^24 tiles of 64 x 64 on; M times a pitch may pass 2^32).  Base pointers need the alignment of
+ * their elements; fastest with 16-byte aligned pointers and K and pitches that are multiples of 8.
  * `workspace`: device scratch of at least hb_linear_workspace_size(M, N, K) bytes, 256-byte aligned, contents undefined on
  * exit; concurrent calls need their own.  The size is 0, and the pointer may be NULL, where the sum over k is not split.
  */
@@ -417,6 +417,8 @@ hb_status hb_linear_valu(const hb_half *x, const hb_half *w, const hb_half *bias
  * out may be x itself with its strides (in place).  positions: int32, positions[b * pos_batch + l * pos_token + a], pos_batch 0
  * shares them between batches.  freq: P fp32 values, DEVICE memory.  sections: `axes` values, HOST memory, read before the
  * call returns; 1 <= axes <= HB_ROPE_MAX_AXES, sections[a] >= 0, 1 <= P <= D / 2.  B, L, H >= 1, 2 <= D <= 65536.
+ * Tokens are turned 16 bytes of each head at a time, or a pair at a time where rows are not aligned: from 2^32 of these on
+ * (B * L times those of a token) HB_ERR_UNSUPPORTED.
  * The angle is reduced to one turn before it is rounded: its error is about 2^-24 of a turn at positions up to 2^24 and
  * 2^-19 at 2^31, beside that of freq itself.
  * Fastest with 16-byte aligned rows (pointers and strides multiples of 8 elements, P a multiple of 8, or of 4 for interleaved).
@@ -436,7 +438,8 @@ hb_status hb_rope_axes(const hb_half *x, hb_half *out, const int32_t *positions,
  * q, out: B x Lq x Hq x D fp16, k, v: B x Lk x Hkv x D fp16, the last axis dense, the others with strides in elements, any order;
  * Hq a multiple of Hkv, D a multiple of 8, at most HB_ATTENTION_MAX_D (HB_ERR_UNSUPPORTED otherwise).  All strides multiples of 8
  * and pointers 16-byte aligned; token strides of k and v at most 2^20, Lk and Lq * (Hq / Hkv) at most 2^31 - 256 (HB_ERR_UNSUPPORTED
- * beyond; other offsets may pass 2^32).
+ * beyond; other offsets may pass 2^32).  B * Hkv * ceil(Lq * (Hq / Hkv) / 128) is less than 2^24, for the twin B * Hq * Lq less than 2^26
+ * (HB_ERR_UNSUPPORTED).
  * Scores, maximum and sum are fp32; the weights exp(s - max) are rounded to fp16 for the product with v.
  * `workspace`: device scratch of at least hb_attention_workspace_size(...) bytes, 256-byte aligned, contents undefined on
  * exit; concurrent calls need their own.  The size is 0, and the pointer may be NULL, where the keys are not split.

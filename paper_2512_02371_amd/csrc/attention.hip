@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(256) attention_valu_kernel(AttentionArgs p) {
 // exchange with lane c + 32, and the weights, rounded to fp16, are in place as the operand of O^T = V^T P^T, whose contraction runs
 // over the keys in the order that the lanes hold them.  V^T is read from LDS by transposing reads.
 constexpr int kAttRows = 32, kAttWaves = 4, kAttTile = kAttRows * kAttWaves;
+constexpr int kAttThreads = 64 * kAttWaves;               // of a workgroup, at least
 
 // A tile of keys in LDS: rows of PC 16-byte pieces (8 up to 64 channels, else 16), a piece at place piece ^ flip: what the fragments' reads
 // take at one time (16 rows of one piece of k; 4 rows of 64 bytes of v) lies in different banks.
@@ -471,8 +472,8 @@ static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_
 
 template <int DP, int GROUPS, bool PARTS>
 static hb_status attention_launch(const AttentionArgs& a, hipStream_t st) {
+    if (!launch_holds(attention_workgroups(a.B, a.Lq, a.Hq, a.Hkv) * a.nparts, 64 * kAttWaves * GROUPS)) return HB_ERR_UNSUPPORTED;
     const int64_t wgs = (int64_t)a.B * a.Hkv * attention_tiles(a.Lq, a.group) * a.nparts;
-    if (wgs > 0x7fffffff) return HB_ERR_UNSUPPORTED;
     const auto kernel = attention_mfma_kernel<DP, GROUPS, PARTS>;
     constexpr int kLds = kAttLds<DP, GROUPS>;
     if (kLds > 32768)
@@ -501,6 +502,7 @@ static hb_status attention_run(const AttentionArgs& a, hipStream_t st) {
 
 extern "C" size_t hb_attention_workspace_size(int B, int Lq, int Lk, int Hq, int Hkv, int D) {
     if (B < 1 || Lq < 1 || Lk < 1 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv != 0 || (int64_t)Lq * (Hq / Hkv) > hb::kAttMost || Lk > hb::kAttMost) return 0;
+    if (!hb::launch_holds(hb::attention_workgroups(B, Lq, Hq, Hkv), hb::kAttThreads)) return 0;
     return hb::attention_workspace(B, Lq, Lk, Hq, Hkv, D);
 }
 
@@ -508,8 +510,8 @@ extern "C" hb_status hb_attention_valu(HB_ATTENTION_PARAMS) {
     using namespace hb;
     AttentionArgs a;
     if (hb_status s = HB_ATTENTION_PREPARE(a)) return s;
+    if (!launch_holds(((double)B * Hq * Lq + 3.0) / 4.0, 256)) return HB_ERR_UNSUPPORTED;
     const int64_t blocks = ((int64_t)B * Hq * Lq + 3) / 4;
-    if (blocks > 0x7fffffff) return HB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(attention_valu_kernel, dim3((unsigned)blocks), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
     return launch_status();
 }
@@ -518,6 +520,7 @@ extern "C" hb_status hb_attention(HB_ATTENTION_PARAMS) {
     using namespace hb;
     AttentionArgs a;
     if (hb_status s = HB_ATTENTION_PREPARE(a)) return s;
+    if (!launch_holds(attention_workgroups(B, Lq, Hq, Hkv), kAttThreads)) return HB_ERR_UNSUPPORTED;
     const auto st = reinterpret_cast<hipStream_t>(stream);
     const AttentionPlan plan = attention_plan(B, Lq, Lk, Hq, Hkv, D);
     if (plan.parts == 1) return plan.groups > 1 ? attention_run<2, false>(a, st) : attention_run<1, false>(a, st);

@@ -11,6 +11,8 @@ constexpr int kAttMost = 0x7fffff00;
 
 // Workgroups (128 rows each) per key head.
 inline int64_t attention_tiles(int Lq, int group) { return ((int64_t)Lq * group + 127) / 128; }
+// Workgroups of one part of the keys; in double, where no sizes overflow.
+inline double attention_workgroups(int B, int Lq, int Hq, int Hkv) { return (double)B * Hkv * (double)attention_tiles(Lq, Hq / Hkv); }
 
 struct AttentionPlan {
     int parts;                    // of the keys, in workgroups of their own; a second launch joins them

@@ -144,6 +144,9 @@ inline int num_cu() {
     return n > 0 ? n : 256;
 }
 
+// HIP takes fewer than 2^32 threads along an axis of a launch.  In double: products of a caller's sizes can pass 64 bits.
+inline bool launch_holds(double workgroups, int threads) { return workgroups * threads < 4294967296.0; }
+
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 }  // namespace hb

@@ -661,7 +661,9 @@ static hb_status linear_launch_large(const LinearArgs& a, hipStream_t st) {
 template <class O, int BM, int BN, int WM, int WN, LinRows ROWS, int G>
 static hb_status linear_launch(const LinearArgs& a, int parts, hipStream_t st) {
     const int64_t tiles = (int64_t)ceil_div(a.M, BM) * ceil_div(a.N, BN);
-    if (tiles > 0x7fffffff) return HB_ERR_UNSUPPORTED;
+    constexpr int kThreads = 64 * (BM / WM) * (BN / WN);
+    static_assert(kThreads == (BM == 128 && BN == 64 ? kLinThreads[kLinTile128x64] : BM == 64 ? kLinThreads[kLinTile64] : kLinThreads[kLinTile128]));
+    if (!launch_holds((double)tiles, kThreads)) return HB_ERR_UNSUPPORTED;
     auto kernel = linear_mfma_kernel<O, BM, BN, WM, WN, ROWS, G>;
     // one step needs one stage, and twice as many workgroups are on a compute unit (1M x 64, K 64, residual: 101 -> 93 us)
     const int kStages = (BM + BN) * 128 * std::min(a.steps > G ? 2 * G : G, a.steps);
@@ -669,7 +671,7 @@ static hb_status linear_launch(const LinearArgs& a, int parts, hipStream_t st) {
     const int kLds = kStages > kPatches ? kStages : kPatches;
     if (kLds > 65536)
         if (hb_status s = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds)) return s;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, parts), dim3(64 * (BM / WM) * (BN / WN)), kLds, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, parts), dim3(kThreads), kLds, st, a);
     return launch_status();
 }
 
@@ -743,7 +745,7 @@ extern "C" hb_status hb_linear_valu(const hb_half* x, const hb_half* w, const hb
     LinearArgs a;
     if (hb_status s = linear_prepare(a, x, w, bias, residual, out, out_type, act, M, N, K, x_pitch, w_pitch, residual_pitch, out_pitch)) return s;
     const int64_t tiles = (int64_t)ceil_div(M, kLvT) * ceil_div(N, kLvT);
-    if (tiles > 0x7fffffff) return HB_ERR_UNSUPPORTED;
+    if (!launch_holds((double)tiles, 256)) return HB_ERR_UNSUPPORTED;
     const auto st = reinterpret_cast<hipStream_t>(stream);
     if (out_type == HB_F32) hipLaunchKernelGGL(linear_valu_kernel<float>, dim3((unsigned)tiles), dim3(256), 0, st, a);
     else hipLaunchKernelGGL(linear_valu_kernel<half_t>, dim3((unsigned)tiles), dim3(256), 0, st, a);

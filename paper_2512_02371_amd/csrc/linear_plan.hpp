@@ -33,6 +33,7 @@ constexpr LinCost kLinCost[kLinKernels] = {
     {64, 64, 0, 0.353, 0.219, 1.29, 0.77, 0.40},  {128, 64, 0, 0.452, 0.358, 2.69, 1.55, 1.11}, {128, 128, 0, 0.528, 0.410, 1.63, 1.35, 0.00},
     {256, 256, 0, 0.744, 1.149, 9.12, 9.24, 0.00},
 };
+constexpr int kLinThreads[kLinKernels] = {1024, 512, 512, 512, 256, 512, 256};                // of a workgroup
 // 64 x 64 copied to LDS directly, 128 x 128 through registers; what one step alone, with half of the LDS, takes of 128 x 64.
 constexpr LinCost kLinCostTile64Copied = {64, 64, 0, 0.240, 0.184, 0.27, 0.60, 0.00}, kLinCostTile128Held = {128, 128, 0, 0.802, 0.296, 2.45, 2.90, 0.34};
 constexpr double kLinOneStep = 0.72;
@@ -67,6 +68,7 @@ inline LinPlan linear_plan(int M, int N, int K, LinRows rows) {
         if (c.waves ? M > c.m || (i > 0 && M <= kLinCost[i - 1].m) : M <= 32) continue;         // few rows have their kernel
         if (kernel == kLinTile256 && (rows != kLinCopied || M <= 128 || N <= 128)) continue;
         const int64_t wgs = (((int64_t)M + c.m - 1) / c.m) * (((int64_t)N + c.n - 1) / c.n);
+        if (kernel != kLinTile256 && wgs >= ((int64_t)1 << 32) / kLinThreads[i]) continue;      // more than a launch holds; the large tile's workgroups stay
         constexpr int kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
         for (int parts : kParts) {
             if (parts > 1 && (kernel == kLinTile256 || wgs * parts > 1024 || steps < (c.waves ? 8 : 2) * parts)) break;

@@ -132,10 +132,11 @@ static hb_status rope_launch(RopeArgs a, hipStream_t st) {
     constexpr int W = INTERLEAVED ? 2 * V : V;
     const int64_t per_token = a.P / V + (a.D - 2 * a.P + W - 1) / W;
     // heads are shared out until there are 16 waves a SIMD to come and go (4: 64 us for 24960 tokens, 24 heads of 128, 57 with 16)
+    if (!launch_holds((double)a.B * a.L * per_token, 1)) return HB_ERR_UNSUPPORTED;
     const int64_t threads = a.B * (int64_t)a.L * per_token, wanted = (int64_t)num_cu() * 4096;
     a.groups = (int)std::min<int64_t>(a.H, std::max<int64_t>(1, wanted / threads));
     const int64_t blocks = (threads * a.groups + 255) / 256;
-    if (blocks > 0x7fffffff) return HB_ERR_UNSUPPORTED;
+    if (!launch_holds((double)blocks, 256)) return HB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((rope_kernel<V, INTERLEAVED>), dim3((unsigned)blocks), dim3(256), 0, st, a);
     return launch_status();
 }

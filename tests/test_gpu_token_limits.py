@@ -24,3 +24,32 @@ def test_as_many_keys_as_a_call_takes():
             assert torch.equal(out, v)
         else:                                             # 2048 of 2^31 keys are missing in the sums and in the weights alike
             assert (out - v).abs().max() <= 2.0 ** -10 * 8.0
+
+
+def test_just_under_2_to_the_32_threads():
+    """2^24 - 8 workgroups of 256 threads, one for each key head: one key each, so that every query's result is its value."""
+    import torch
+    B, H, D = (1 << 21) - 1, 8, 8
+    q = torch.ones((1, 1, H, D), dtype=torch.float16, device="cuda:0").expand(B, 1, H, D)
+    v = torch.randn((B, 1, H, D), device="cuda:0").half()
+    out = torch.full_like(v, 7.0)
+    print("hb_attention", B, flush=True)
+    hb.hb_attention(q, v, v, out, 1.0)
+    torch.cuda.synchronize()
+    assert torch.equal(out, v)
+
+
+def test_rope_just_under_2_to_the_32_threads():
+    """2^32 - 2^16 pairs at odd strides: each by itself, all of them a half turn."""
+    import torch
+    B, L = (1 << 16) - 1, 1 << 16
+    token = 3                                             # elements from token to token: two of them turn, the third is between
+    x = torch.zeros((B * L * token,), dtype=torch.float16, device="cuda:0")
+    x[0::token], x[1::token], x[2::token] = 1.0, -2.0, 7.0
+    view = x.as_strided((B, L, 1, 2), (L * token, token, 2, 1))
+    pos = torch.ones((1, 1, 1), dtype=torch.int32, device="cuda:0").expand(B, L, 1)
+    print("hb_rope_axes", B, L, flush=True)
+    hb.hb_rope_axes(view, view, pos, torch.full((1,), 3.14159265, device="cuda:0"), [1])
+    torch.cuda.synchronize()
+    for i, want in enumerate((-1.0, 2.0, 7.0)):
+        assert bool((x[i::token] == want).all()), i
