@@ -416,7 +416,8 @@ hb_status hb_linear_valu(const hb_half *x, const hb_half *w, const hb_half *bias
  * transpose, which is also the gradient).  x, out: B x L x H x D fp16, the last axis dense, the others with strides in elements;
  * out may be x itself with its strides (in place).  positions: int32, positions[b * pos_batch + l * pos_token + a], pos_batch 0
  * shares them between batches.  freq: P fp32 values, DEVICE memory.  sections: `axes` values, HOST memory, read before the
- * call returns; 1 <= axes <= HB_ROPE_MAX_AXES, sections[a] >= 0, 1 <= P <= D / 2.  B, L, H >= 1, 2 <= D <= 65536.
+ * call returns; 1 <= axes <= HB_ROPE_MAX_AXES, sections[a] >= 0, 1 <= P <= D / 2.  B, L, H >= 1, 2 <= D <= 65536, H at most
+ * 2^31 - 2^20 (HB_ERR_UNSUPPORTED beyond).
  * Tokens are turned 16 bytes of each head at a time, or a pair at a time where rows are not aligned: from 2^32 of these on
  * (B * L times those of a token) HB_ERR_UNSUPPORTED.
  * The angle is reduced to one turn before it is rounded: its error is about 2^-24 of a turn at positions up to 2^24 and

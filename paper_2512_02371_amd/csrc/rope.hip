@@ -6,6 +6,9 @@
 
 namespace hb {
 
+// Threads that share a token's heads, at most, and the heads that a loop over them can count in 32 bits.
+constexpr int kRopeMostGroups = 1 << 20, kRopeMostHeads = 0x7fffffff - kRopeMostGroups + 1;
+
 struct RopeArgs {
     const half_t* x;
     half_t* out;
@@ -102,7 +105,7 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs p) {
         }
     };
     int h = group;
-    for (; h + (U - 1) * p.groups < p.H; h += U * p.groups) {
+    for (const int last = p.H - (U - 1) * p.groups; h < last; h += U * p.groups) {
         vec a[U], c[U];
 #pragma unroll
         for (int i = 0; i < U; ++i) {
@@ -134,7 +137,7 @@ static hb_status rope_launch(RopeArgs a, hipStream_t st) {
     // heads are shared out until there are 16 waves a SIMD to come and go (4: 64 us for 24960 tokens, 24 heads of 128, 57 with 16)
     if (!launch_holds((double)a.B * a.L * per_token, 1)) return HB_ERR_UNSUPPORTED;
     const int64_t threads = a.B * (int64_t)a.L * per_token, wanted = (int64_t)num_cu() * 4096;
-    a.groups = (int)std::min<int64_t>(a.H, std::max<int64_t>(1, wanted / threads));
+    a.groups = (int)std::min<int64_t>(std::min(a.H, kRopeMostGroups), std::max<int64_t>(1, wanted / threads));
     const int64_t blocks = (threads * a.groups + 255) / 256;
     if (!launch_holds((double)blocks, 256)) return HB_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((rope_kernel<V, INTERLEAVED>), dim3((unsigned)blocks), dim3(256), 0, st, a);
@@ -151,7 +154,7 @@ extern "C" hb_status hb_rope_axes(const hb_half* x, hb_half* out, const int32_t*
     if (!aligned_to(x, 2) || !aligned_to(out, 2) || !aligned_to(positions, 4) || !aligned_to(freq, 4)) return HB_ERR_INVALID_ARG;
     for (int64_t s : {x_batch, x_token, x_head, out_batch, out_token, out_head, pos_batch, pos_token})
         if (s < 0) return HB_ERR_INVALID_ARG;
-    if (axes > HB_ROPE_MAX_AXES || D > 65536) return HB_ERR_UNSUPPORTED;
+    if (axes > HB_ROPE_MAX_AXES || D > 65536 || H > kRopeMostHeads) return HB_ERR_UNSUPPORTED;
     RopeArgs a = {reinterpret_cast<const half_t*>(x), reinterpret_cast<half_t*>(out), positions, freq, B, L, H, D, 0,
                   x_batch, x_token, x_head, out_batch, out_token, out_head, pos_batch, pos_token, {}, interleaved != 0, 1};
     int64_t pairs = 0;

@@ -96,3 +96,11 @@ def test_linear_takes_a_kernel_whose_launch_holds_the_rows(tmp_path):
         for kernel in map(int, kernels.split()):
             m, n, size = workgroup[kernel]
             assert -(-M // m) * -(-N // n) * size < 1 << 32, (M, N, K, kernel)
+
+
+@pytest.mark.parametrize("H", [(1 << 31) - (1 << 20) + 1, (1 << 31) - 1])
+def test_rope_heads_that_the_loop_cannot_count(lib, H):
+    """A thread goes on by four times the threads of a token at most (2^20): beyond 2^31 - 2^20 heads that passed 32 bits, and the place became negative."""
+    sections = (ctypes.c_int32 * 1)(1)
+    for stride in (0, 1, 8):
+        assert lib.hb_rope_axes(P, P, P, P, 1, 1, H, 2, 0, 0, stride, 0, 0, stride, 0, 0, sections, 1, 0, None) == UNSUPPORTED
