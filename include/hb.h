@@ -93,7 +93,7 @@ typedef enum {
     HB_ACT_GELU = 2,          /* v (1 + erf(v / sqrt 2)) / 2 */
     HB_ACT_GELU_TANH = 3,     /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
     HB_ACT_SILU = 4           /* v / (1 + exp(-v)) */
-} hb_act;
+} hb_act;                     /* relative errors, far tails included: gelu 2^-20 + v^2 2^-23, gelu_tanh 2^-20 + |z| 2^-20 (tanh z), silu 2^-20 + |v| 2^-22 */
 
 /* Human-readable name of a status code (static storage). */
 const char *hb_status_string(hb_status s);
