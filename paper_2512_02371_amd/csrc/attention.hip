@@ -451,15 +451,20 @@ __global__ void __launch_bounds__(256) attention_join_kernel(AttentionArgs p) {
 }
 
 static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_half* k, const hb_half* v, hb_half* out, int B, int Lq, int Lk,
-                                   int Hq, int Hkv, int D, const int64_t (&st)[12], float scale, const int32_t* key_len,
+                                   int Hq, int Hkv, int D, const int64_t (&strides)[12], float scale, const int32_t* key_len,
                                    const uint8_t* key_mask, int64_t mask_pitch) {
     if (!q || !out || (Lk > 0 && (!k || !v))) return HB_ERR_INVALID_ARG;
     if (B < 1 || Lq < 1 || Lk < 0 || Hq < 1 || Hkv < 1 || D < 1 || Hq % Hkv != 0) return HB_ERR_INVALID_ARG;
     if (!isfinite(scale) || !aligned_to(key_len, 4)) return HB_ERR_INVALID_ARG;
     for (const void* x : {(const void*)q, (const void*)k, (const void*)v, (const void*)out})
         if (!aligned_to(x, 16)) return HB_ERR_INVALID_ARG;
-    for (int64_t s : st)
-        if (s < 0 || s % 8 != 0) return HB_ERR_INVALID_ARG;
+    // batch, token and head strides of q, k, v, out; that of a single batch, token or head has no meaning
+    const int sizes[12] = {B, Lq, Hq, B, Lk, Hkv, B, Lk, Hkv, B, Lq, Hq};
+    int64_t st[12];
+    for (int i = 0; i < 12; ++i) {
+        st[i] = sizes[i] > 1 ? strides[i] : 0;
+        if (st[i] < 0 || st[i] % 8 != 0) return HB_ERR_INVALID_ARG;
+    }
     if (key_mask && mask_pitch < 0) return HB_ERR_INVALID_ARG;
     if (D % 8 != 0 || D > HB_ATTENTION_MAX_D) return HB_ERR_UNSUPPORTED;
     if (st[4] > (1 << 20) || st[7] > (1 << 20) || (int64_t)Lq * (Hq / Hkv) > kAttMost || Lk > kAttMost) return HB_ERR_UNSUPPORTED;
