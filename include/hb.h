@@ -413,8 +413,8 @@ hb_status hb_linear_valu(const hb_half *x, const hb_half *w, const hb_half *bias
  *     t = positions[b][l][axis of p] * freq[p]
  *     (u, v) -> (u cos t - v sin t, v cos t + u sin t)
  * Pair p is channels (p, P + p), or (2p, 2p + 1) where `interleaved` is not 0.  Negated frequencies turn back (the
- * transpose, which is also the gradient).  x, out: B x L x H x D fp16, the last axis dense, the others with strides in elements;
- * out may be x itself with its strides (in place).  positions: int32, positions[b * pos_batch + l * pos_token + a], pos_batch 0
+ * transpose, which is also the gradient).  x, out: B x L x H x D fp16, the last axis dense, the others with strides in elements
+ * (that of a dimension of size 1 has no meaning, here and in positions); out may be x itself with its strides (in place).  positions: int32, positions[b * pos_batch + l * pos_token + a], pos_batch 0
  * shares them between batches.  freq: P fp32 values, DEVICE memory.  sections: `axes` values, HOST memory, read before the
  * call returns; 1 <= axes <= HB_ROPE_MAX_AXES, sections[a] >= 0, 1 <= P <= D / 2.  B, L, H >= 1, 2 <= D <= 65536, H at most
  * 2^31 - 2^20 (HB_ERR_UNSUPPORTED beyond).

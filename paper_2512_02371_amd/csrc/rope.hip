@@ -152,6 +152,10 @@ extern "C" hb_status hb_rope_axes(const hb_half* x, hb_half* out, const int32_t*
     using namespace hb;
     if (!x || !out || !positions || !freq || !sections || B < 1 || L < 1 || H < 1 || D < 2 || axes < 1) return HB_ERR_INVALID_ARG;
     if (!aligned_to(x, 2) || !aligned_to(out, 2) || !aligned_to(positions, 4) || !aligned_to(freq, 4)) return HB_ERR_INVALID_ARG;
+    // the stride of a single batch, token or head has no meaning, and must not decide how wide the accesses are
+    if (B == 1) x_batch = out_batch = pos_batch = 0;
+    if (L == 1) x_token = out_token = pos_token = 0;
+    if (H == 1) x_head = out_head = 0;
     for (int64_t s : {x_batch, x_token, x_head, out_batch, out_token, out_head, pos_batch, pos_token})
         if (s < 0) return HB_ERR_INVALID_ARG;
     if (axes > HB_ROPE_MAX_AXES || D > 65536 || H > kRopeMostHeads) return HB_ERR_UNSUPPORTED;

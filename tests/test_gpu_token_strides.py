@@ -40,3 +40,26 @@ def test_rope(interleaved, shape, dims):
     print("hb_rope_axes", shape, interleaved, flush=True)
     hb.hb_rope_axes(odd(x, dims, 3), odd(out, dims, 5), pos, freq, [32], interleaved)
     assert torch.equal(out, want)
+
+
+def test_rope_keeps_its_wide_accesses():
+    """A million tokens of one image and one head, the strides of both odd: 2-byte accesses take twice as long (65 and 150 us)."""
+    import torch
+    x = torch.randn((1, 1000000, 1, 64), device="cuda:0").half()
+    pos = torch.zeros((1, 1000000, 1), dtype=torch.int32, device="cuda:0")
+    freq, out = torch.rand(32, device="cuda:0"), torch.empty_like(x)
+
+    def least(a, b):
+        times = []
+        for _ in range(6):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(5):
+                hb.hb_rope_axes(a, b, pos, freq, [32])
+            end.record()
+            end.synchronize()
+            times.append(start.elapsed_time(end))
+        return min(times)
+    usual, other = least(x, out), least(odd(x, (0, 2), 3), odd(out, (0, 2), 3))
+    print("five calls", usual, "ms; odd strides", other, "ms", flush=True)
+    assert other < 1.5 * usual
