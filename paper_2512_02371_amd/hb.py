@@ -472,8 +472,15 @@ def hb_pyr_level_valu(inp, residual, down=None):
     return _pyr("hb_pyr_level_valu", inp, residual, down)
 
 
+def _ints(*sizes):
+    """Sizes as the library takes them: ctypes would pass the low 32 bits of larger ones."""
+    n = [int(s) for s in sizes]
+    assert max(n) <= 0x7fffffff, "sizes below 2^31 expected"
+    return n
+
+
 def hb_linear_workspace_size(M, N, K):
-    return int(load().hb_linear_workspace_size(int(M), int(N), int(K)))
+    return int(load().hb_linear_workspace_size(*_ints(M, N, K)))
 
 
 def _scratch(t):
@@ -490,6 +497,7 @@ def _linear(name, x, w, out, workspace, bias, residual, act):
     assert out.dtype in (torch.float16, torch.float32), "fp16 or fp32 output expected"
     po, Mo, No, op = _img2d(out, out.dtype)
     assert K == Kw and (Mo, No) == (M, N), "x: M x K, w: N x K, out: M x N"
+    _ints(M, N, K)
     pb = pr = None
     rp = N
     if bias is not None:
@@ -523,6 +531,7 @@ def _heads(t):
     """B x L x H x D, the last axis dense -> (address, (B, L, H, D), strides of the first three)."""
     s = t.stride()
     assert t.is_cuda and t.dtype == torch.float16 and len(s) == 4 and (s[3] == 1 or t.shape[3] == 1), "B x L x H x D fp16 CUDA tensor expected"
+    _ints(*t.shape)
     return t.data_ptr(), t.shape, s[:3]
 
 
@@ -543,7 +552,7 @@ def hb_rope_axes(x, out, positions, freq, sections, interleaved=False):
 
 
 def hb_attention_workspace_size(B, Lq, Lk, Hq, Hkv, D):
-    return int(load().hb_attention_workspace_size(int(B), int(Lq), int(Lk), int(Hq), int(Hkv), int(D)))
+    return int(load().hb_attention_workspace_size(*_ints(B, Lq, Lk, Hq, Hkv, D)))
 
 
 def _attention(name, q, k, v, out, scale, workspace, key_len, key_mask):

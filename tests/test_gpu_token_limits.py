@@ -53,3 +53,21 @@ def test_rope_just_under_2_to_the_32_threads():
     torch.cuda.synchronize()
     for i, want in enumerate((-1.0, 2.0, 7.0)):
         assert bool((x[i::token] == want).all()), i
+
+
+def test_sizes_beyond_an_int_are_not_cut_off():
+    """2^32 + 5 keys, broadcast: not a call of five keys.  2^32 + 3 rows: not a call of three."""
+    import torch
+    q = torch.ones((1, 2, 1, 8), dtype=torch.float16, device="cuda:0")
+    k = q[:, :1].expand(1, (1 << 32) + 5, 1, 8)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda:0")
+    for fn in (hb.hb_attention, hb.hb_attention_valu):
+        with pytest.raises(AssertionError):
+            fn(q, k, k, torch.empty_like(q), 1.0, ws)
+    x = torch.zeros(((1 << 32) + 3, 1), dtype=torch.float16, device="cuda:0")
+    for fn in (hb.hb_linear, hb.hb_linear_valu):
+        with pytest.raises(AssertionError):
+            fn(x, x[:1], x, ws)
+    pos, turns = torch.zeros((1, 1, 1), dtype=torch.int32, device="cuda:0"), x.view(-1)[: (1 << 32) + 2].view(1, (1 << 31) + 1, 1, 2)
+    with pytest.raises(AssertionError):
+        hb.hb_rope_axes(turns, turns, pos.expand(1, (1 << 31) + 1, 1), torch.ones(1, device="cuda:0"), [1])

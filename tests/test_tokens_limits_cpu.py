@@ -104,3 +104,13 @@ def test_rope_heads_that_the_loop_cannot_count(lib, H):
     sections = (ctypes.c_int32 * 1)(1)
     for stride in (0, 1, 8):
         assert lib.hb_rope_axes(P, P, P, P, 1, 1, H, 2, 0, 0, stride, 0, 0, stride, 0, 0, sections, 1, 0, None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("n", [1 << 31, (1 << 32) + 1, (1 << 40) + 64])
+def test_sizes_beyond_an_int_are_not_cut_off(lib, n):
+    """A size goes to the library as an int: what does not fit must not arrive as its low 32 bits."""
+    for f, args in ((hb.hb_linear_workspace_size, (64, 512, 8192)), (hb.hb_attention_workspace_size, (1, 1, 16384, 8, 1, 128))):
+        assert f(*args) > 0
+        for i in range(len(args)):
+            with pytest.raises(AssertionError):
+                f(*args[:i], n, *args[i + 1:])
