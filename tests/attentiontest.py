@@ -1,0 +1,11 @@
+"""Calls of hb_attention that between them take every kernel that its choice by size takes: B, Lq, Lk, Hq, Hkv, D."""
+
+FORMS = [(2, 150, 130, 4, 2, 24), (3, 3, 517, 2, 1, 16), (2, 3, 300, 2, 1, 24), (2, 3, 12300, 2, 2, 24),
+         (2, 150, 130, 4, 2, 40), (3, 3, 517, 2, 1, 48), (2, 3, 130, 2, 1, 56), (2, 3, 4100, 2, 1, 40),
+         (2, 150, 130, 4, 2, 72), (3, 3, 517, 2, 1, 80), (2, 3, 130, 2, 1, 88), (2, 3, 4100, 2, 1, 72),
+         (3, 3, 130, 2, 1, 104), (3, 3, 517, 2, 1, 112), (2, 3, 300, 2, 1, 120), (2, 3, 12300, 2, 1, 104)]
+
+
+def instance(parts, groups, D):
+    """(channels rounded up to 32, groups of waves, whether the keys are split): what is compiled apart."""
+    return (D + 31) // 32 * 32, groups, parts > 1
