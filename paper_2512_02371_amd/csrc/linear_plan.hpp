@@ -22,7 +22,9 @@ struct LinPlan {
 // The time of a call in us, as a model with a few constants per kernel: a workgroup alone on a compute unit takes `alone` a step and
 // `begin` beside it, one of several `shared` and `end`; a kernel for few rows of x has its waves take turns at the steps.  `odd`:
 // what rows at odd addresses add.  The constants were fitted to 1200 calls of random sizes (1 .. 2^20 x 16 .. 8192, K 16 ..
-// 8192), each timed with every kernel and with 1 to 32 parts: the choice is on average 0.9 % behind the fastest.
+// 8192; fp16 output, no residual), each timed with every kernel and with 1 to 32 parts; `odd` of 64 x 64 was set anew when that kernel came to
+// move its odd rows behind the products.  On 1200 other calls, of the kernels as they are now, the choice is on average 1.1 % behind the fastest.
+// fp32 output and residuals are not in the model: with both of them it is 2.5 % behind, and up to 38 % where N is below 50.
 struct LinCost {
     int m, n;                     // outputs of a workgroup
     int waves;                    // that share the steps; 0: tiles
@@ -34,7 +36,10 @@ constexpr LinCost kLinCost[kLinKernels] = {
     {256, 256, 0, 0.744, 1.149, 9.12, 9.24, 0.00},
 };
 constexpr int kLinThreads[kLinKernels] = {1024, 512, 512, 512, 256, 512, 256};                // of a workgroup
-// 64 x 64 copied to LDS directly, 128 x 128 through registers; what one step alone, with half of the LDS, takes of 128 x 64.
+// 64 x 64 copied to LDS directly, 128 x 128 through registers.  A call of one step has one stage of LDS, and more workgroups on a compute unit; only
+// 128 x 64 gains by it, by kLinOneStep.  261 calls of K up to 64 took, in the median and in terms of the model without it, 0.81 (rows at even
+// addresses) and 0.87 (odd) with 128 x 64, 1.00 and 1.05 with 64 x 64, 0.97 and 0.99 with 128 x 128, 0.95 with 256 x 256; the choice among them
+// is 1.3 % behind the fastest with it, 2.9 % without (K from 65 to 128: 0.7 %).
 constexpr LinCost kLinCostTile64Copied = {64, 64, 0, 0.240, 0.184, 0.27, 0.60, 0.00}, kLinCostTile128Held = {128, 128, 0, 0.802, 0.296, 2.45, 2.90, 0.34};
 constexpr double kLinOneStep = 0.72;
 constexpr double kLinLaunch = 2.5, kLinJoin = 2.58, kLinJoinPart = 0.28, kLinJoinRate = 6.9e6;      // us, us, us, bytes per us
