@@ -112,12 +112,6 @@ __device__ __forceinline__ int attention_place(int wg, int nwg, int same) {
 // (8 x 4096 x 77, 16 heads 37 us of 22 for the bytes); one query, memory (4 x 16384 keys, 8 heads of 128: 36 us, 4.7 TB/s, and the join).
 // Products of the next tile ahead of the weights gain 1 to 6 % with many keys and lose with few; a third stage of LDS gains nothing.
 //
-// The weights are rounded to fp16 for their product with v, which makes a result's error 1.4 times that of its own rounding (2.9e-4 of its
-// root mean square in place of 2.1e-4).  A second product with what the rounding left over would take that away: where keys are many it
-// costs 30 to 35 % (4 x 4096 x 4096, 16 heads of 64: 307 -> 415 us; 3 x 1079 x 1917, 12 heads over 4 of 80: 47 -> 62), with up to 128 keys 5 to
-// 11 % (8 x 4096 x 77: 41.4 -> 44.6), and is left out; where the keys are split the matrix units wait for memory (4 x 1 x 16384, 32 heads over 8
-// of 128: 56.2 -> 57.2; 8 x 1 x 8192, 8 heads of 64: 33.4 -> 34.0; 2 x 4 x 16384, 40 over 4 of 128, the dearest found: 22.4 -> 24.2), and it is there.
-//
 // D rounded up to DP; PARTS: the sums go to the workspace.  GROUPS 2: eight waves, four for the even tiles of the keys and four for the odd
 // ones, each with tiles of its own in LDS; they join their sums there.  A workgroup that has a compute unit to itself is done in half the time.
 template <int DP, int GROUPS, bool PARTS>
@@ -126,7 +120,6 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
     constexpr int kPitch = 16 * PC, kMatrix = 64 * kPitch, kStage = 2 * kMatrix;      // bytes: a row, a tile of k or v, both
     constexpr int kOwn = PC / 4, kRowsOf = 64 / PC;                                    // copies of 1 KB per matrix and wave, rows in one
     constexpr int kOutPitch = 2 * DP + 16;                                             // bytes of a row on its way out
-    constexpr int kTerms = PARTS ? 2 : 1;                                              // products of v with the weights
     static_assert(kAttLds<DP, GROUPS> >= GROUPS * 2 * kStage && kAttLds<DP, GROUPS> >= kAttTile * kOutPitch);
     extern __shared__ __attribute__((aligned(1024))) char s_all[];
     __shared__ __attribute__((aligned(16))) float s_hide[GROUPS][2][64];               // of the tiles with hidden keys: 0, or -inf for these
@@ -238,7 +231,7 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
                 for (int j = 0; j < 16; ++j) s[k][j] = 0.f;
             score();
         }
-        half8 w[kTerms][4];
+        half8 w[4];
         half4 vf[2][kBlocks];                                 // of the first 16 keys: on their way while the weights are computed
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
@@ -258,23 +251,8 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
             for (int j = 0; j < 4; ++j) part[j] = e[0][j];
 #pragma unroll
             for (int j = 4; j < 32; ++j) part[j % 4] += e[j / 16][j % 16];
-            if constexpr (kTerms == 1) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) w[0][j / 8][j % 8] = (half_t)e[j / 16][j % 16];
-            } else {                                          // truncated, so that the rest is exact in fp32
-                typedef half_t half2v __attribute__((ext_vector_type(2)));
-#pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    const float a = e[j / 16][j % 16], b = e[j / 16][j % 16 + 1];
-                    const half2v most = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(a, b));
-                    const half2v rest = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(a - (float)most[0], b - (float)most[1]));
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        w[0][j / 8][j % 8 + i] = most[i];
-                        w[kTerms - 1][j / 8][j % 8 + i] = rest[i];
-                    }
-                }
-            }
+            for (int j = 0; j < 32; ++j) w[j / 8][j % 8] = (half_t)e[j / 16][j % 16];
         };
         bool redo = careful;
         if (!careful) {
@@ -323,9 +301,7 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
                 }
             }
 #pragma unroll
-            for (int term = 0; term < kTerms; ++term)
-#pragma unroll
-                for (int i = 0; i < kBlocks; ++i) o[i] = mfma32x32x16(v[i], w[term][k], o[i]);
+            for (int i = 0; i < kBlocks; ++i) o[i] = mfma32x32x16(v[i], w[k], o[i]);
         }
     };
 
