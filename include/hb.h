@@ -441,7 +441,8 @@ hb_status hb_rope_axes(const hb_half *x, hb_half *out, const int32_t *positions,
  * (that of a dimension of size 1 has no meaning) and pointers 16-byte aligned; token strides of k and v at most 2^20, Lk and
  * Lq * (Hq / Hkv) at most 2^31 - 256 (HB_ERR_UNSUPPORTED beyond; other offsets may pass 2^32).  B * Hkv * ceil(Lq * (Hq / Hkv) / 128)
  * is less than 2^24, for the twin B * Hq * Lq less than 2^26 (HB_ERR_UNSUPPORTED).
- * Scores, maximum and sum are fp32; the weights exp(s - max) are rounded to fp16 for the product with v.
+ * Scores, maximum and sum are fp32; the weights exp(s - max) are rounded to fp16 for the product with v, to 20 bits where the keys
+ * are split (where the workspace's size is not 0) and Lq * (Hq / Hkv) is at most 32, as for single tokens.
  * `workspace`: device scratch of at least hb_attention_workspace_size(...) bytes, 256-byte aligned, contents undefined on
  * exit; concurrent calls need their own.  The size is 0, and the pointer may be NULL, where the keys are not split.
  */

@@ -112,14 +112,22 @@ __device__ __forceinline__ int attention_place(int wg, int nwg, int same) {
 // (8 x 4096 x 77, 16 heads 37 us of 22 for the bytes); one query, memory (4 x 16384 keys, 8 heads of 128: 36 us, 4.7 TB/s, and the join).
 // Products of the next tile ahead of the weights gain 1 to 6 % with many keys and lose with few; a third stage of LDS gains nothing.
 //
+// The weights are rounded to fp16 for their product with v, which makes a result's error 1.4 times that of its own rounding (2.9e-4 of its
+// root mean square in place of 2.1e-4).  TERMS 2: a second product with what the rounding left over takes that away.  Where keys are many it
+// costs 30 to 35 % (4 x 4096 x 4096, 16 heads of 64: 307 -> 415 us; 3 x 1079 x 1917, 12 heads over 4 of 80: 47 -> 62), with up to 128 keys 5 to
+// 11 % (8 x 4096 x 77: 41.4 -> 44.6), and is left out.  With split keys and rows of one wave, the form of single tokens, the units wait for
+// memory for most of the time, and it is there: 1 to 8 %, 5 % in the mean of 144 calls (4 x 1 x 16384, 32 heads over 8 of 128: 53.6 -> 54.5;
+// 8 x 1 x 8192, 8 heads of 64: 33.4 -> 33.6; 4 x 2 x 5000, 8 heads of 80: 15.4 -> 16.5).
+//
 // D rounded up to DP; PARTS: the sums go to the workspace.  GROUPS 2: eight waves, four for the even tiles of the keys and four for the odd
 // ones, each with tiles of its own in LDS; they join their sums there.  A workgroup that has a compute unit to itself is done in half the time.
-template <int DP, int GROUPS, bool PARTS>
+template <int DP, int GROUPS, bool PARTS, int TERMS>
 __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_kernel(AttentionArgs p) {
     constexpr int PC = DP <= 64 ? 8 : 16, kSteps = DP / 16, kBlocks = DP / 32;
     constexpr int kPitch = 16 * PC, kMatrix = 64 * kPitch, kStage = 2 * kMatrix;      // bytes: a row, a tile of k or v, both
     constexpr int kOwn = PC / 4, kRowsOf = 64 / PC;                                    // copies of 1 KB per matrix and wave, rows in one
     constexpr int kOutPitch = 2 * DP + 16;                                             // bytes of a row on its way out
+    static_assert(TERMS == 1 || TERMS == 2);
     static_assert(kAttLds<DP, GROUPS> >= GROUPS * 2 * kStage && kAttLds<DP, GROUPS> >= kAttTile * kOutPitch);
     extern __shared__ __attribute__((aligned(1024))) char s_all[];
     __shared__ __attribute__((aligned(16))) float s_hide[GROUPS][2][64];               // of the tiles with hidden keys: 0, or -inf for these
@@ -231,7 +239,7 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
                 for (int j = 0; j < 16; ++j) s[k][j] = 0.f;
             score();
         }
-        half8 w[4];
+        half8 w[TERMS][4];
         half4 vf[2][kBlocks];                                 // of the first 16 keys: on their way while the weights are computed
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
@@ -251,8 +259,23 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
             for (int j = 0; j < 4; ++j) part[j] = e[0][j];
 #pragma unroll
             for (int j = 4; j < 32; ++j) part[j % 4] += e[j / 16][j % 16];
+            if constexpr (TERMS == 1) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) w[j / 8][j % 8] = (half_t)e[j / 16][j % 16];
+                for (int j = 0; j < 32; ++j) w[0][j / 8][j % 8] = (half_t)e[j / 16][j % 16];
+            } else {                                          // truncated, so that the rest is exact in fp32
+                typedef half_t half2v __attribute__((ext_vector_type(2)));
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                    const float a = e[j / 16][j % 16], b = e[j / 16][j % 16 + 1];
+                    const half2v most = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(a, b));
+                    const half2v rest = __builtin_bit_cast(half2v, __builtin_amdgcn_cvt_pkrtz(a - (float)most[0], b - (float)most[1]));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        w[0][j / 8][j % 8 + i] = most[i];
+                        w[TERMS - 1][j / 8][j % 8 + i] = rest[i];
+                    }
+                }
+            }
         };
         bool redo = careful;
         if (!careful) {
@@ -301,7 +324,9 @@ __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_ker
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kBlocks; ++i) o[i] = mfma32x32x16(v[i], w[k], o[i]);
+            for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+                for (int i = 0; i < kBlocks; ++i) o[i] = mfma32x32x16(v[i], w[term][k], o[i]);
         }
     };
 
@@ -475,23 +500,27 @@ static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_
     return HB_OK;
 }
 
-template <int DP, int GROUPS, bool PARTS>
+template <int DP, int GROUPS, bool PARTS, int TERMS>
 static hb_status attention_launch(const AttentionArgs& a, hipStream_t st) {
     if (!launch_holds(attention_workgroups(a.B, a.Lq, a.Hq, a.Hkv) * a.nparts, 64 * kAttWaves * GROUPS)) return HB_ERR_UNSUPPORTED;
     const int64_t wgs = (int64_t)a.B * a.Hkv * attention_tiles(a.Lq, a.group) * a.nparts;
-    const auto kernel = attention_mfma_kernel<DP, GROUPS, PARTS>;
+    const auto kernel = attention_mfma_kernel<DP, GROUPS, PARTS, TERMS>;
     constexpr int kLds = kAttLds<DP, GROUPS>;
     if (kLds > 32768)
         if (hb_status s = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds)) return s;
     hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(64 * kAttWaves * GROUPS), kLds, st, a);
     return launch_status();
 }
-template <int GROUPS, bool PARTS>
+template <int GROUPS, bool PARTS, int TERMS>
 static hb_status attention_run(const AttentionArgs& a, hipStream_t st) {
-    if (a.D <= 32) return attention_launch<32, GROUPS, PARTS>(a, st);
-    if (a.D <= 64) return attention_launch<64, GROUPS, PARTS>(a, st);
-    if (a.D <= 96) return attention_launch<96, GROUPS, PARTS>(a, st);
-    return attention_launch<128, GROUPS, PARTS>(a, st);
+    if (a.D <= 32) return attention_launch<32, GROUPS, PARTS, TERMS>(a, st);
+    if (a.D <= 64) return attention_launch<64, GROUPS, PARTS, TERMS>(a, st);
+    if (a.D <= 96) return attention_launch<96, GROUPS, PARTS, TERMS>(a, st);
+    return attention_launch<128, GROUPS, PARTS, TERMS>(a, st);
+}
+template <bool PARTS, int TERMS>
+static hb_status attention_run(int groups, const AttentionArgs& a, hipStream_t st) {
+    return groups > 1 ? attention_run<2, PARTS, TERMS>(a, st) : attention_run<1, PARTS, TERMS>(a, st);
 }
 
 }  // namespace hb
@@ -528,11 +557,12 @@ extern "C" hb_status hb_attention(HB_ATTENTION_PARAMS) {
     if (!launch_holds(attention_workgroups(B, Lq, Hq, Hkv), kAttThreads)) return HB_ERR_UNSUPPORTED;
     const auto st = reinterpret_cast<hipStream_t>(stream);
     const AttentionPlan plan = attention_plan(B, Lq, Lk, Hq, Hkv, D);
-    if (plan.parts == 1) return plan.groups > 1 ? attention_run<2, false>(a, st) : attention_run<1, false>(a, st);
+    if (plan.parts == 1) return attention_run<false, 1>(plan.groups, a, st);
     if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < attention_workspace(B, Lq, Lk, Hq, Hkv, D)) return HB_ERR_WORKSPACE;
     a.nparts = plan.parts;
     a.parts = static_cast<float*>(workspace);
-    if (hb_status s = plan.groups > 1 ? attention_run<2, true>(a, st) : attention_run<1, true>(a, st)) return s;
+    const bool one_wave = (int64_t)Lq * a.group <= kAttRows;
+    if (hb_status s = one_wave ? attention_run<true, 2>(plan.groups, a, st) : attention_run<true, 1>(plan.groups, a, st)) return s;
     const int64_t blocks = ((int64_t)B * Hq * Lq + 3) / 4;
     hipLaunchKernelGGL(attention_join_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
     return launch_status();

@@ -27,7 +27,7 @@ def test_every_form_is_tested(tmp_path):
 
     def taken(calls):
         out = subprocess.run([str(tmp_path / "plan")], input="\n".join("%d %d %d %d %d %d" % c for c in calls), capture_output=True, text=True, check=True).stdout
-        return {instance(*map(int, l.split()), c[5]) for c, l in zip(calls, out.splitlines())}
+        return {instance(*map(int, l.split()), c[1], *c[3:]) for c, l in zip(calls, out.splitlines())}
     rng = random.Random(1)
     size = lambda most: max(1, int(most ** rng.random()))
     calls = []
@@ -35,4 +35,4 @@ def test_every_form_is_tested(tmp_path):
         Hkv = size(32)
         calls.append((size(64), size(1 << 13), size(1 << 15), Hkv * size(16), Hkv, 8 * rng.randint(1, 16)))
     reached, tested = taken(calls), taken(FORMS)
-    assert len(reached) >= 12 and reached <= tested, sorted(reached - tested)
+    assert len(reached) >= 20 and reached <= tested, sorted(reached - tested)
