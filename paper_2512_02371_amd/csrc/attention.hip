@@ -108,8 +108,10 @@ __device__ __forceinline__ int attention_place(int wg, int nwg, int same) {
 }
 
 // What bounds it, by size (queries x keys, heads of 64 unless said): many keys, the power of matrix and vector units together (4 x 4096 x 4096, 16 heads
-// 310 us, 880 TFLOP/s at 1.8 GHz, 0.42 and 0.58 busy); few keys, a workgroup's chain from its queries to its rows, with two on a compute unit
-// (8 x 4096 x 77, 16 heads 37 us of 22 for the bytes); one query, memory (4 x 16384 keys, 8 heads of 128: 36 us, 4.7 TB/s, and the join).
+// 312 us, 880 TFLOP/s at 2.0 GHz, 0.42 and 0.59 busy); few keys, a workgroup's chain from its queries to its rows, with two on a compute unit
+// (8 x 4096 x 77, 16 heads 37.5 us of 22 for the bytes); one query, memory (4 x 16384 keys, 8 heads of 128: 39 us, 4.9 TB/s, and the join).
+// LDS conflicts are those of the rows on their way out, 192 cycles a workgroup whatever the keys: 0.22 of all cycles of LDS with 77 keys,
+// where these are few, and 2 % of a workgroup's time.
 // Products of the next tile ahead of the weights gain 1 to 6 % with many keys and lose with few; a third stage of LDS gains nothing.
 //
 // The weights are rounded to fp16 for their product with v, which makes a result's error 1.4 times that of its own rounding (2.9e-4 of its
@@ -120,7 +122,7 @@ __device__ __forceinline__ int attention_place(int wg, int nwg, int same) {
 // 8 x 1 x 8192, 8 heads of 64: 33.4 -> 33.6; 4 x 2 x 5000, 8 heads of 80: 15.4 -> 16.5).
 //
 // D rounded up to DP; PARTS: the sums go to the workspace.  GROUPS 2: eight waves, four for the even tiles of the keys and four for the odd
-// ones, each with tiles of its own in LDS; they join their sums there.  A workgroup that has a compute unit to itself is done in half the time.
+// ones, each with tiles of its own in LDS; they join their sums there.  A workgroup that has a compute unit to itself takes about two thirds of the time.
 template <int DP, int GROUPS, bool PARTS, int TERMS>
 __global__ void __launch_bounds__(64 * kAttWaves * GROUPS, 2) attention_mfma_kernel(AttentionArgs p) {
     constexpr int PC = DP <= 64 ? 8 : 16, kSteps = DP / 16, kBlocks = DP / 32;

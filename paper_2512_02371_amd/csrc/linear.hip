@@ -114,8 +114,9 @@ __device__ __forceinline__ half8 lin_last8(const half_t* row, int k, int K) {
     return r;
 }
 
-// `count` of V adjacent elements, at any address that their type allows.  Stores are streaming: whole lines of a row leave at a time (8192 x 8192, K
-// 2048: 236 -> 228 us; 100000 x 200 fp32, K 96: 62 -> 43).
+// `count` of V adjacent elements, at any address that their type allows.  Stores are streaming, whole lines of a row at a time, which is for what
+// they would push out of the caches: 100000 x 200 fp32, K 96, with a residual 48 -> 38 us, but 23 -> 33 without one; 2^20 x 64, K 64 with a residual
+// 83.8 -> 82.5; 8192 x 8192, K 2048 with gelu_tanh 245 -> 243, without 234 -> 238; smaller outputs within 5 %.
 template <int V, class T>
 __device__ __forceinline__ void lin_load(float (&v)[V], const T* from, int count) {
     typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
@@ -252,7 +253,8 @@ __device__ __forceinline__ void lin_tile(int wg, int tiles_m, int tiles_n, int& 
 //
 // A lone workgroup of 64 x 64 is bound by the chain of a step (barrier, reads from LDS, products): two steps behind one barrier (1024 x 1024,
 // K 1024 8.3 -> 7.2 us; 1920 x 1088, K 1024 11.8 -> 9.9), and more stages without that gain nothing.  Of 128 x 128 two workgroups share a compute
-// unit instead.  Rows that are not copied pass through registers (1917 x 1079, K 1023 16.4 us), where a second step gains nothing.
+// unit instead.  Rows that are not copied pass through registers (1917 x 1079, K 1023 15.3 us, 16.8 with silu and an fp32 residual; K 1024,
+// copied, 11.8), where a second step gains nothing.
 // Few k are bound by memory (1M x 64, K 64 with residual: 80 us, 5.0 TB/s); odd rows by their loads, two or three for 16 bytes.
 template <class O, int BM, int BN, int WM, int WN, LinRows ROWS, int G>
 __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_kernel(LinearArgs p) {
@@ -396,7 +398,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
             if (s + 1 < steps) put((s + 1) & 1, TkInt<0>{});
         }
     } else {
-        // odd rows are moved behind the products, so that these need not wait for them (1917 x 1079, K 1023 19.2 -> 16.4 us; with more rows a wave, in
+        // odd rows are moved behind the products, so that these need not wait for them (1917 x 1079, K 1023, no activation 19.2 -> 16.4 us; with more rows a wave, in
         // the larger tiles, that is slower: 4000 x 4001, K 2001 119 -> 124)
         const int whole = min(steps, K / kLinK);
         if (whole > 0) {
@@ -432,9 +434,8 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
 // what eight waves of 128 x 64 would read), and nothing but its own products hides these reads: while the 64 products of one half of a
 // stage run, the fragments of the next half are on their way, one read or copy between two products.  A workgroup stays and takes tile
 // after tile, and the first two stages of the next tile are copied while the last one's results leave.
-// 8192 x 8192, K 2048 with gelu: 244 us, 1.13 PFLOP/s at the 2.0 GHz that its power leaves, the matrix units busy for 0.49 of the time (tiles
-// of 128 x 128 293 us); 4096 x 4096, K 4096 113 us (137).  Each round of tiles costs some 9 us beside its products: below K of about 2000 the smaller
-// tiles are as fast.
+// 8192 x 8192, K 2048 with gelu_tanh: 243 us, 1.13 PFLOP/s at the 2.2 GHz that its power leaves, the matrix units busy for 0.48 of the time (tiles
+// of 128 x 128 280 us); 4096 x 4096, K 4096 111 us (131), K 2048 61 (69), K 1024 35 (40).  Each round of tiles costs some 9 us beside its products.
 constexpr int kLinLargeLds = 160 * 1024;                                    // two stages of 64 KB and 8 KB of patch a wave
 template <class O>
 __global__ void __launch_bounds__(256, 1) linear_large_kernel(LinearArgs p) {
