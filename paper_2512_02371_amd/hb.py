@@ -491,11 +491,18 @@ def _scratch(t):
     return t.data_ptr(), t.numel()
 
 
+def _rows(t, dtype):
+    """As _img2d; the stride from column to column of a single one has no meaning."""
+    if t.dim() == 2 and t.shape[1] == 1:
+        t = t.as_strided(t.shape, (t.stride(0), 1))
+    return _img2d(t, dtype)
+
+
 def _linear(name, x, w, out, workspace, bias, residual, act):
-    px, M, K, xp = _img2d(x, torch.float16)
-    pw, N, Kw, wp = _img2d(w, torch.float16)
+    px, M, K, xp = _rows(x, torch.float16)
+    pw, N, Kw, wp = _rows(w, torch.float16)
     assert out.dtype in (torch.float16, torch.float32), "fp16 or fp32 output expected"
-    po, Mo, No, op = _img2d(out, out.dtype)
+    po, Mo, No, op = _rows(out, out.dtype)
     assert K == Kw and (Mo, No) == (M, N), "x: M x K, w: N x K, out: M x N"
     _ints(M, N, K)
     pb = pr = None
@@ -504,7 +511,7 @@ def _linear(name, x, w, out, workspace, bias, residual, act):
         assert bias.is_cuda and bias.dtype == torch.float16 and bias.shape == (N,) and bias.is_contiguous(), "bias: N"
         pb = bias.data_ptr()
     if residual is not None:
-        pr, Mr, Nr, rp = _img2d(residual, out.dtype)
+        pr, Mr, Nr, rp = _rows(residual, out.dtype)
         assert (Mr, Nr) == (M, N), "residual: M x N"
     pws, nws = _scratch(workspace)
     if M == 1:                                    # the pitch of a single row has no meaning, and torch gives any

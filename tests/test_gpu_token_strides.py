@@ -63,3 +63,16 @@ def test_rope_keeps_its_wide_accesses():
     usual, other = least(x, out), least(odd(x, (0, 2), 3), odd(out, (0, 2), 3))
     print("five calls", usual, "ms; odd strides", other, "ms", flush=True)
     assert other < 1.5 * usual
+
+
+@pytest.mark.parametrize("fn", ["hb_linear", "hb_linear_valu"])
+def test_linear_of_one_column(fn):
+    """K = 1 and N = 1: the stride from column to column has no meaning."""
+    import torch
+    x, w = torch.randn((1, 200), device="cuda:0").half(), torch.randn((1, 70), device="cuda:0").half()
+    want = x.t().float() @ w.float()
+    out = getattr(hb, fn)(x.t(), w.t(), torch.empty((200, 70), dtype=torch.float32, device="cuda:0"))
+    assert torch.equal(out, want)                         # one product each
+    column, beside = (torch.full((1, 200), 7.0, device="cuda:0").t() for _ in range(2))
+    getattr(hb, fn)(x.t(), w[:, :1], column, residual=beside)
+    assert torch.equal(column, want[:, :1] + 7.0)
