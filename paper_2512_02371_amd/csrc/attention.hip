@@ -497,8 +497,9 @@ static hb_status attention_prepare(AttentionArgs& a, const hb_half* q, const hb_
     if (st[4] > (1 << 20) || st[7] > (1 << 20) || (int64_t)Lq * (Hq / Hkv) > kAttMost || Lk > kAttMost) return HB_ERR_UNSUPPORTED;
     a = {reinterpret_cast<const half_t*>(q), reinterpret_cast<const half_t*>(k), reinterpret_cast<const half_t*>(v), reinterpret_cast<half_t*>(out),
          B, Lq, Lk, Hq, Hkv, D, Hq / Hkv, st[0], st[1], st[2], st[3], st[4], st[5], st[6], st[7], st[8], st[9], st[10], st[11],
-         // a scale of 0 as one that is too small to tell: hidden scores are -inf, and that times 0 is no number
-         fmaxf(fabsf(scale) * 1.44269504f, 1e-30f), scale < 0.f, key_len, key_mask, mask_pitch, nullptr, 1};
+         // a scale of 0 as one that is too small to tell: hidden scores are -inf, and that times 0 is no number; nor are scores of 0 times
+         // infinity, which the largest scales would become
+         fminf(fmaxf(fabsf(scale) * 1.44269504f, 1e-30f), FLT_MAX), scale < 0.f, key_len, key_mask, mask_pitch, nullptr, 1};
     return HB_OK;
 }
 

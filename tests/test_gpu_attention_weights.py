@@ -32,3 +32,15 @@ def test_split_keys(B, Lq, Lk, Hq, Hkv, D, keys):
     once = rms(want.astype(np.float16).astype(np.float64) - want)
     got = rms(out.double().cpu().numpy() - want)
     assert want.size >= 2000 and got <= 1.1 * once, (got / once, got / rms(want))
+
+
+@pytest.mark.parametrize("fn", ["hb_attention", "hb_attention_valu"])
+@pytest.mark.parametrize("scale", [3.0e38, -3.0e38, 3.4028234e38])
+def test_scales_near_the_largest_number(fn, scale):
+    """Scores of 0 stay 0: the scale in powers of two (1.44 times as large) must not become infinite."""
+    import torch
+    q = torch.zeros((1, 3, 2, 64), dtype=torch.float16, device="cuda:0")
+    k, v = (torch.randn((1, 100, 2, 64), device="cuda:0").half() for _ in range(2))
+    out = getattr(hb, fn)(q, k, v, torch.empty_like(q), scale)
+    want = v.double().mean(dim=1, keepdim=True).expand(1, 3, 2, 64)
+    assert ((out.double() - want).abs() <= 2.0 ** -10 * v.double().abs().mean(dim=1, keepdim=True)).all()
