@@ -52,7 +52,7 @@
  *    None of it depends on the data of a call.
  *  - Every stage has a `_valu` twin with the same signature and results that uses
  *    only vector-ALU FMAs (no MFMA): the ablation that shows what the matrix units
- *    buy.  (hb_rope_axes, which has no product, has none.)
+ *    buy.  (hb_rope_axes, hb_group_norm and hb_quantize_rows, which have no product, have none.)
  */
 #ifndef HB_H
 #define HB_H
@@ -79,14 +79,16 @@ typedef void *hb_stream;      /* hipStream_t */
 #define HB_MAX_TAPS_FIR1D 256   /* hb_fir1d: the large-tap regime of Sec. V-A */
 #define HB_MAX_TAPS_CONV2D 32   /* per axis, hb_conv2d, hb_down2, hb_up2 */
 #define HB_RESIZE_MAX_SPAN 512   /* hb_resize: largest band */
-#define HB_LINEAR_MAX_PITCH (1 << 21)   /* hb_linear: elements between two rows */
+#define HB_LINEAR_MAX_PITCH (1 << 21)   /* hb_linear, hb_linear_i8: elements between two rows */
+#define HB_LINEAR_I8_MAX_K 131071       /* hb_linear_i8: the sum of that many products of 8-bit integers holds in 32 bits */
+#define HB_GROUP_NORM_MAX_CHANNELS 4096 /* hb_group_norm: channels of a group */
 #define HB_ATTENTION_MAX_D 128   /* hb_attention: channels of a head */
 #define HB_ROPE_MAX_AXES 4       /* hb_rope_axes */
 
-/* Element types of hb_linear's output and residual. */
+/* Element types of the output and residual of hb_linear and hb_linear_i8, of the input and output of hb_group_norm. */
 typedef enum { HB_F16 = 0, HB_F32 = 1 } hb_type;
 
-/* Activations of hb_linear. */
+/* Activations of hb_linear, hb_linear_i8 and hb_group_norm. */
 typedef enum {
     HB_ACT_NONE = 0,
     HB_ACT_RELU = 1,          /* max(v, 0) */
@@ -457,6 +459,53 @@ hb_status hb_attention_valu(const hb_half *q, const hb_half *k, const hb_half *v
                             int64_t v_batch, int64_t v_token, int64_t v_head, int64_t out_batch, int64_t out_token, int64_t out_head,
                             float scale, const int32_t *key_len_or_null, const uint8_t *key_mask_or_null, int64_t mask_pitch,
                             void *workspace, size_t workspace_bytes, hb_stream stream);
+
+/*
+ * Group norm with an activation, channels last.  The C channels of a pixel are `groups` groups of D = C / groups neighbours; with mean and
+ * var over the P pixels of image n and the D channels of the group of c (var the mean of the squares of x - mean):
+ *     out[n][p][c] = act((x[n][p][c] - mean) / sqrt(var + eps) * weight[c] + bias[c])
+ * x, out: N images of P pixels of C channels, fp16 or fp32 each, the channels adjacent, x[n * x_image + p * x_pixel + c] (strides in elements, at least C,
+ * in any order; that of a single image or pixel has no meaning).  out may be x itself, of one type and with its strides (in place).
+ * weight, bias: C fp16 values, or NULL for ones and zeros.  eps > 0.  groups 1 is a norm over whole images, and with P = 1 over the channels of each token.
+ * Statistics are fp32, the variance of the differences from the mean (a mean far from zero costs no digits of it but those of the mean itself); one
+ * rounding at the end.  A NaN or an infinity makes NaN of its image's group alone.  fp32 values must be such that the sum of the squares of a group's differences holds in fp32.
+ * N, P, C >= 1; D at most HB_GROUP_NORM_MAX_CHANNELS, P and N * groups less than 2^30 (HB_ERR_UNSUPPORTED beyond; offsets may pass 2^32).  Base pointers need the
+ * alignment of their elements; fastest with 16-byte aligned pixels.
+ * `workspace`: device scratch of at least hb_group_norm_workspace_size(N, P, C, groups) bytes, 256-byte aligned, contents undefined on exit; concurrent
+ * calls need their own.  The size is 0, and the pointer may be NULL, where the pixels of a group fit a compute unit.
+ */
+size_t hb_group_norm_workspace_size(int N, int P, int C, int groups);
+hb_status hb_group_norm(const void *x, hb_type x_type, const hb_half *weight_or_null, const hb_half *bias_or_null, void *out, hb_type out_type,
+                        hb_act act, float eps, int N, int P, int C, int groups, int64_t x_image, int64_t x_pixel, int64_t out_image,
+                        int64_t out_pixel, void *workspace, size_t workspace_bytes, hb_stream stream);
+
+/*
+ * Rows as 8-bit integers, for hb_linear_i8: activations token by token, weights (N x K) channel by channel.
+ *     scale[m] = max_k |x[m][k]| / 127,   q[m][k] = round(127 x[m][k] / max_k |x[m][k]|)   (ties to even)
+ * The integers are those of the exact quotients, -127 .. 127; the scale is the fp32 number nearest to its quotient.  A row of zeros has scale 0 and zeros, a row with a NaN or
+ * an infinity scale NaN and zeros.  x: M x K fp16, q: M x K int8, scale: M fp32.  M, K >= 1; pitches in elements, >= K (that of a single row has no
+ * meaning); M less than 2^24 (HB_ERR_UNSUPPORTED beyond).  Base pointers need the alignment of their elements; fastest with 16-byte aligned
+ * rows of x and 8-byte aligned rows of q.
+ */
+hb_status hb_quantize_rows(const hb_half *x, int8_t *q, float *scale, int M, int K, int64_t x_pitch, int64_t q_pitch, hb_stream stream);
+
+/*
+ * hb_linear in 8-bit integers, with a scale for each row of both operands:
+ *     out[m][n] = act(x_scale[m] * w_scale[n] * sum_{k < K} x[m][k] w[n][k] + bias[n]) + residual[m][n]
+ * x: M x K int8, w: N x K int8 (-128 too), x_scale: M fp32, w_scale: N fp32, bias: N fp16 or NULL, residual and out: M x N of out_type, residual may be NULL or
+ * `out` itself with its pitch (in place).  The sum is exact, in 32-bit integers; it is rounded to fp32 and times x_scale[m], then w_scale[n]; these, the bias, the
+ * activation and the residual are fp32 and rounded once, to out_type.  A scale that is NaN makes NaN of its row or column alone.  M, N, K >= 1, K at most HB_LINEAR_I8_MAX_K;
+ * pitches in elements, >= the row, at most HB_LINEAR_MAX_PITCH, M at most 2^31 - 256 (HB_ERR_UNSUPPORTED beyond, and for the twin from 2^24 tiles of 64 x 64 on).
+ * Base pointers need the alignment of their elements; fastest with 16-byte aligned x and w, K and pitches that are multiples of 16.
+ * `workspace`: as hb_linear's, of hb_linear_i8_workspace_size(M, N, K) bytes.
+ */
+size_t hb_linear_i8_workspace_size(int M, int N, int K);
+hb_status hb_linear_i8(const int8_t *x, const int8_t *w, const float *x_scale, const float *w_scale, const hb_half *bias_or_null,
+                       const void *residual_or_null, void *out, hb_type out_type, hb_act act, int M, int N, int K, int64_t x_pitch,
+                       int64_t w_pitch, int64_t residual_pitch, int64_t out_pitch, void *workspace, size_t workspace_bytes, hb_stream stream);
+hb_status hb_linear_i8_valu(const int8_t *x, const int8_t *w, const float *x_scale, const float *w_scale, const hb_half *bias_or_null,
+                            const void *residual_or_null, void *out, hb_type out_type, hb_act act, int M, int N, int K, int64_t x_pitch,
+                            int64_t w_pitch, int64_t residual_pitch, int64_t out_pitch, void *workspace, size_t workspace_bytes, hb_stream stream);
 
 /*
  * Measurement helper, not a stage: out[i] = (float) in[i] for n elements with 16-byte

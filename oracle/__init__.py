@@ -393,3 +393,51 @@ def attention(q, k, v, scale, key_len=None, key_mask=None):
             e = np.exp(s - s.max(axis=1, keepdims=True))
             out[b, :, h] = (e @ v[b, seen, hk]) / e.sum(axis=1, keepdims=True)
     return out
+
+
+def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none"):
+    """act((x - mean) / sqrt(var + eps) * weight + bias), mean and var over the pixels and the channels of a group; x [N, P, C]."""
+    x = np.asarray(x, dtype=np.float64)
+    N, P, C = x.shape
+    out = np.empty((N, P, C))
+    D = C // groups
+    for n in range(N):
+        for g in range(groups):
+            v = x[n, :, g * D:(g + 1) * D]
+            d = v - v.mean()
+            out[n, :, g * D:(g + 1) * D] = d / np.sqrt((d * d).mean() + eps)
+    if weight is not None:
+        out = out * np.asarray(weight, dtype=np.float64)
+    if bias is not None:
+        out = out + np.asarray(bias, dtype=np.float64)
+    return activation(out, act)
+
+
+def quantize_rows(x):
+    """(integers, scales): 127 x / max |x| of each row to the nearest integer, ties to even, by whole numbers; max |x| / 127.  fp16 rows."""
+    x = np.asarray(x)
+    assert x.dtype == np.float16
+    units = (x.astype(np.float64) * 2.0 ** 24)                          # whole numbers: 2^-24 is the smallest fp16 value
+    q, scale = np.zeros(x.shape, dtype=np.int8), np.zeros(len(x))
+    for m in range(len(x)):
+        if not np.isfinite(units[m]).all():
+            scale[m] = np.nan
+            continue
+        u = units[m].astype(np.int64)
+        top = int(np.abs(u).max())
+        scale[m] = top * 2.0 ** -24 / 127.0
+        if top:
+            whole, rest = np.divmod(127 * np.abs(u), top)
+            up = (2 * rest > top) | ((2 * rest == top) & (whole % 2 == 1))
+            q[m] = np.sign(u) * (whole + up)
+    return q, scale
+
+
+def linear_i8(x, w, x_scale, w_scale, bias=None, residual=None, act="none"):
+    """act(x_scale[m] w_scale[n] sum_k x[m][k] w[n][k] + bias[n]) + residual[m][n], the sum exact."""
+    s = np.asarray(x, dtype=np.float64) @ np.asarray(w, dtype=np.float64).T                # whole numbers below 2^53: exact
+    v = s * np.asarray(x_scale, dtype=np.float64)[:, None] * np.asarray(w_scale, dtype=np.float64)[None, :]
+    if bias is not None:
+        v = v + np.asarray(bias, dtype=np.float64)[None, :]
+    v = activation(v, act)
+    return v if residual is None else v + residual

@@ -29,9 +29,11 @@ HB_MAX_TAPS = 64            # per axis, hb_sepblur
 HB_MAX_TAPS_FIR1D = 256     # hb_fir1d
 HB_MAX_TAPS_CONV2D = 32     # per axis, hb_conv2d
 HB_LINEAR_MAX_PITCH = 1 << 21
+HB_LINEAR_I8_MAX_K = 131071
+HB_GROUP_NORM_MAX_CHANNELS = 4096
 HB_ATTENTION_MAX_D = 128
 HB_ROPE_MAX_AXES = 4
-HB_ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}      # hb_linear
+HB_ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}      # hb_linear, hb_linear_i8, hb_group_norm
 
 # every symbol include/hb.h declares
 SYMBOLS = [
@@ -49,6 +51,9 @@ SYMBOLS = [
     "hb_linear_workspace_size", "hb_linear", "hb_linear_valu",
     "hb_rope_axes",
     "hb_attention_workspace_size", "hb_attention", "hb_attention_valu",
+    "hb_group_norm_workspace_size", "hb_group_norm",
+    "hb_quantize_rows",
+    "hb_linear_i8_workspace_size", "hb_linear_i8", "hb_linear_i8_valu",
     "hb_copy_f16_f32", "hb_mfma_probe",
 ]
 
@@ -122,11 +127,13 @@ def load() -> ctypes.CDLL:
     lin = [vp, vp, vp, vp, vp, I, I, I, I, I, I64, I64, I64, I64, vp, ctypes.c_size_t, vp]
     att = [vp, vp, vp, vp, I, I, I, I, I, I] + [I64] * 12 + [ctypes.c_float, vp, vp, I64, vp, ctypes.c_size_t, vp]
     for name, sig in (("hb_linear", lin), ("hb_linear_valu", lin), ("hb_attention", att), ("hb_attention_valu", att),
-                      ("hb_rope_axes", [vp, vp, vp, vp, I, I, I, I] + [I64] * 8 + [vp, I, I, vp])):
+                      ("hb_rope_axes", [vp, vp, vp, vp, I, I, I, I] + [I64] * 8 + [vp, I, I, vp]),
+                      ("hb_group_norm", [vp, I, vp, vp, vp, I, I, ctypes.c_float, I, I, I, I, I64, I64, I64, I64, vp, ctypes.c_size_t, vp]),
+                      ("hb_quantize_rows", [vp, vp, vp, I, I, I64, I64, vp]), ("hb_linear_i8", [vp, vp] + lin), ("hb_linear_i8_valu", [vp, vp] + lin)):
         f = getattr(L, name)
         f.argtypes = sig
         f.restype = I
-    for name, n in (("hb_linear_workspace_size", 3), ("hb_attention_workspace_size", 6)):
+    for name, n in (("hb_linear_workspace_size", 3), ("hb_attention_workspace_size", 6), ("hb_group_norm_workspace_size", 4), ("hb_linear_i8_workspace_size", 3)):
         f = getattr(L, name)
         f.argtypes = [I] * n
         f.restype = ctypes.c_size_t
@@ -592,6 +599,103 @@ def hb_attention(q, k, v, out, scale, workspace=None, key_len=None, key_mask=Non
 
 def hb_attention_valu(q, k, v, out, scale, workspace=None, key_len=None, key_mask=None):
     return _attention("hb_attention_valu", q, k, v, out, scale, workspace, key_len, key_mask)
+
+
+def _here(*tensors):
+    """The launch goes to the current device."""
+    now = torch.cuda.current_device()
+    assert all(t is None or t.get_device() == now for t in tensors), "tensors on the current device expected"
+
+
+def _per_channel(t, C, what):
+    """Address of C fp16 values; None is none."""
+    if t is None:
+        return None
+    assert t.is_cuda and t.dtype == torch.float16 and t.shape == (C,) and t.is_contiguous(), f"{what}: a contiguous fp16 value per channel"
+    return t.data_ptr()
+
+
+def _pixels(t):
+    """N x P x C or N x H x W x C, the channels dense -> (address, 1 for fp32, (N, P, C), strides of images and pixels)."""
+    assert t.is_cuda and t.dtype in (torch.float16, torch.float32) and t.dim() in (3, 4), "N x P x C or N x H x W x C, fp16 or fp32 CUDA tensor expected"
+    n, s = tuple(t.shape), t.stride()
+    assert s[-1] == 1 or n[-1] == 1, "adjacent channels expected"
+    pixel = s[-2]
+    if len(n) == 4:
+        if n[2] == 1:
+            pixel = s[1]
+        else:
+            assert n[1] == 1 or s[1] == n[2] * pixel, "pixels at one distance expected"
+        n = (n[0], n[1] * n[2], n[3])
+    _ints(*n)
+    return t.data_ptr(), int(t.dtype == torch.float32), n, (s[0], pixel)
+
+
+def hb_group_norm_workspace_size(N, P, C, groups):
+    return int(load().hb_group_norm_workspace_size(*_ints(N, P, C, groups)))
+
+
+def hb_group_norm(x, out, groups, weight=None, bias=None, eps=1e-5, act="none", workspace=None):
+    """out = act((x - mean) / sqrt(var + eps) * weight + bias) by groups of channels; x, out: N x P x C or N x H x W x C, fp16 or fp32; out may be x."""
+    px, tx, (N, P, C), xs = _pixels(x)
+    po, to, _, os_ = _pixels(out)
+    assert out.shape == x.shape, "output shape"
+    _here(x, out, weight, bias, workspace)
+    pws, nws = _scratch(workspace)
+    _check("hb_group_norm", (_lib or load()).hb_group_norm(px, tx, _per_channel(weight, C, "weight"), _per_channel(bias, C, "bias"), po, to, HB_ACTS[act], float(eps),
+                                                           N, P, C, *_ints(groups), *xs, *os_, pws, nws, _stream()))
+    return out
+
+
+def _scales(t, n, what):
+    assert t.is_cuda and t.dtype == torch.float32 and t.shape == (n,) and t.is_contiguous(), f"{what}: a contiguous fp32 value per row"
+    return t.data_ptr()
+
+
+def hb_quantize_rows(x, q, scale):
+    """Rows of x (M x K fp16) as 8-bit integers q (M x K int8) times scale (M fp32)."""
+    px, M, K, xp = _rows(x, torch.float16)
+    pq, Mq, Kq, qp = _rows(q, torch.int8)
+    assert (Mq, Kq) == (M, K), "x, q: M x K"
+    _ints(M, K)
+    _here(x, q, scale)
+    _check("hb_quantize_rows", (_lib or load()).hb_quantize_rows(px, pq, _scales(scale, M, "scale"), M, K, xp, qp, _stream()))
+    return q, scale
+
+
+def hb_linear_i8_workspace_size(M, N, K):
+    return int(load().hb_linear_i8_workspace_size(*_ints(M, N, K)))
+
+
+def _linear_i8(name, x, w, x_scale, w_scale, out, workspace, bias, residual, act):
+    px, M, K, xp = _rows(x, torch.int8)
+    pw, N, Kw, wp = _rows(w, torch.int8)
+    assert out.dtype in (torch.float16, torch.float32), "fp16 or fp32 output expected"
+    po, Mo, No, op = _rows(out, out.dtype)
+    assert K == Kw and (Mo, No) == (M, N), "x: M x K, w: N x K, out: M x N"
+    _ints(M, N, K)
+    _here(x, w, x_scale, w_scale, out, workspace, bias, residual)
+    pr, rp = None, N
+    if residual is not None:
+        pr, Mr, Nr, rp = _rows(residual, out.dtype)
+        assert (Mr, Nr) == (M, N), "residual: M x N"
+    pws, nws = _scratch(workspace)
+    if M == 1:                                    # the pitch of a single row has no meaning, and torch gives any
+        xp, op, rp = K, N, N
+    if N == 1:
+        wp = K
+    _check(name, getattr(_lib or load(), name)(px, pw, _scales(x_scale, M, "x_scale"), _scales(w_scale, N, "w_scale"), _per_channel(bias, N, "bias"), pr, po,
+                                               1 if out.dtype == torch.float32 else 0, HB_ACTS[act], M, N, K, xp, wp, rp, op, pws, nws, _stream()))
+    return out
+
+
+def hb_linear_i8(x, w, x_scale, w_scale, out, workspace=None, bias=None, residual=None, act="none"):
+    """out = act(x_scale w_scale (x w^T) + bias) + residual; x: M x K int8, w: N x K int8, a scale per row of each, out and residual: M x N, fp16 or fp32."""
+    return _linear_i8("hb_linear_i8", x, w, x_scale, w_scale, out, workspace, bias, residual, act)
+
+
+def hb_linear_i8_valu(x, w, x_scale, w_scale, out, workspace=None, bias=None, residual=None, act="none"):
+    return _linear_i8("hb_linear_i8_valu", x, w, x_scale, w_scale, out, workspace, bias, residual, act)
 
 
 def hb_copy_f16_f32(inp, out):
