@@ -118,6 +118,16 @@ __device__ __forceinline__ half8 shift_in_from_left(half8 v, int d) {
     return __builtin_bit_cast(half8, a);
 }
 
+// Byte i becomes byte i + d of the 16, zeros behind them; d >= 0.
+__device__ __forceinline__ u32x4 shift_in_bytes(u32x4 a, int d) {
+    const u32x4 s16 = {0, 0, 0, 0}, s8 = {a[2], a[3], 0, 0};
+    a = d >= 16 ? s16 : (d & 8) ? s8 : a;
+    const u32x4 s4 = {a[1], a[2], a[3], 0};
+    a = (d & 4) ? s4 : a;
+    const uint32_t shift = 8 * (d & 3);
+    return u32x4{__builtin_amdgcn_alignbit(a[1], a[0], shift), __builtin_amdgcn_alignbit(a[2], a[1], shift), __builtin_amdgcn_alignbit(a[3], a[2], shift), a[3] >> shift};
+}
+
 // Store four consecutive floats at row[x .. x+3], dropping columns >= W.
 __device__ __forceinline__ void store4_mask(float* __restrict__ row, int x, int W, floatx4 v) {
     if (x + 4 <= W) {

@@ -1,31 +1,14 @@
 // hb_linear_i8: matrix product in 8-bit integers with a scale for each row of both operands and hb_linear's epilogue, and its vector-ALU twin.
-#include "hb_device.hpp"
-#include "hb_host.hpp"
-#include "token_epilogue.hpp"
+#include "linear_tiles.hpp"
 
 namespace hb {
-
-struct LinearI8Args {
-    const int8_t* x;
-    const int8_t* w;
-    const float* x_scale;
-    const float* w_scale;
-    const half_t* bias;        // null: none
-    const void* residual;      // null: none
-    void* out;
-    int M, N, K, act;
-    int64_t x_pitch, w_pitch, res_pitch, out_pitch;
-};
-
-// A sum of products times its scales; the integer is rounded to 24 bits.
-__device__ __forceinline__ float i8_scaled(int sum, float xs, float ws) { return (float)sum * xs * ws; }
 
 // ---------------------------------------------------------------------------
 // Vector-ALU twin: 64 x 64 outputs per workgroup, 4 x 4 per thread, 16 k at a time through LDS.
 constexpr int kI8vT = 64, kI8vK = 16;
 
 template <class O>
-__global__ void __launch_bounds__(256) linear_i8_valu_kernel(LinearI8Args p) {
+__global__ void __launch_bounds__(256) linear_i8_valu_kernel(LinearArgs<LinI8> p) {
     __shared__ int s_x[kI8vK][kI8vT + 4], s_w[kI8vK][kI8vT + 4];
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int tiles_n = (p.N + kI8vT - 1) / kI8vT;
@@ -50,15 +33,13 @@ __global__ void __launch_bounds__(256) linear_i8_valu_kernel(LinearI8Args p) {
         for (int j = 0; j < 4; ++j) {
             const int m = m0 + 4 * ty + i, n = n0 + 4 * tx + j;
             if (m >= p.M || n >= p.N) continue;
-            float v = linear_act(i8_scaled(acc[i][j], p.x_scale[m], p.w_scale[n]) + (p.bias ? (float)p.bias[n] : 0.f), p.act);
+            float v = linear_act(lin_scaled(acc[i][j], p.x_scale[m], p.w_scale[n]) + (p.bias ? (float)p.bias[n] : 0.f), p.act);
             if (p.residual) v += (float)static_cast<const O*>(p.residual)[m * p.res_pitch + n];
             static_cast<O*>(p.out)[m * p.out_pitch + n] = (O)v;
         }
 }
 
-constexpr int kI8MostRows = 0x7fffff00;                   // row numbers are 32 bits up to the end of the last tile
-
-static hb_status linear_i8_prepare(LinearI8Args& a, const int8_t* x, const int8_t* w, const float* x_scale, const float* w_scale, const hb_half* bias,
+static hb_status linear_i8_prepare(LinearArgs<LinI8>& a, const int8_t* x, const int8_t* w, const float* x_scale, const float* w_scale, const hb_half* bias,
                                    const void* residual, void* out, int out_type, int act, int M, int N, int K, int64_t x_pitch, int64_t w_pitch,
                                    int64_t res_pitch, int64_t out_pitch) {
     if (!x || !w || !x_scale || !w_scale || !out || M < 1 || N < 1 || K < 1) return HB_ERR_INVALID_ARG;
@@ -69,41 +50,37 @@ static hb_status linear_i8_prepare(LinearI8Args& a, const int8_t* x, const int8_
     if (!aligned_to(x_scale, 4) || !aligned_to(w_scale, 4) || !aligned_to(bias, 2) || !aligned_to(residual, size) || !aligned_to(out, size)) return HB_ERR_INVALID_ARG;
     for (int64_t p : {x_pitch, w_pitch, res_pitch, out_pitch})
         if (p > HB_LINEAR_MAX_PITCH) return HB_ERR_UNSUPPORTED;
-    if (M > kI8MostRows || K > HB_LINEAR_I8_MAX_K) return HB_ERR_UNSUPPORTED;
-    a = {x, w, x_scale, w_scale, reinterpret_cast<const half_t*>(bias), residual, out, M, N, K, act, x_pitch, w_pitch, res_pitch, out_pitch};
+    if (M > kLinMostRows || K > HB_LINEAR_I8_MAX_K) return HB_ERR_UNSUPPORTED;
+    a = {x, w, reinterpret_cast<const half_t*>(bias), residual, out, M, N, K, act, x_pitch, w_pitch, res_pitch, out_pitch, (K - 1) / LinI8::kK + 1, x_scale, w_scale};
     return HB_OK;
-}
-
-static hb_status linear_i8_valu(const LinearI8Args& a, int out_type, hipStream_t st) {
-    const int64_t tiles = (int64_t)ceil_div(a.M, kI8vT) * ((a.N - 1) / kI8vT + 1);
-    if (!launch_holds((double)tiles, 256)) return HB_ERR_UNSUPPORTED;
-    if (out_type == HB_F32) hipLaunchKernelGGL(linear_i8_valu_kernel<float>, dim3((unsigned)tiles), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(linear_i8_valu_kernel<half_t>, dim3((unsigned)tiles), dim3(256), 0, st, a);
-    return launch_status();
 }
 
 }  // namespace hb
 
-extern "C" size_t hb_linear_i8_workspace_size(int, int, int) { return 0; }
+extern "C" size_t hb_linear_i8_workspace_size(int M, int N, int K) {
+    return M < 1 || N < 1 || K < 1 ? 0 : hb::linear_workspace(M, N, hb::LinI8::halves(K));
+}
 
 extern "C" hb_status hb_linear_i8_valu(const int8_t* x, const int8_t* w, const float* x_scale, const float* w_scale, const hb_half* bias, const void* residual,
                                        void* out, hb_type out_type, hb_act act, int M, int N, int K, int64_t x_pitch, int64_t w_pitch,
                                        int64_t residual_pitch, int64_t out_pitch, void* workspace, size_t workspace_bytes, hb_stream stream) {
     using namespace hb;
-    (void)workspace;
-    (void)workspace_bytes;
-    LinearI8Args a;
+    LinearArgs<LinI8> a;
     if (hb_status s = linear_i8_prepare(a, x, w, x_scale, w_scale, bias, residual, out, out_type, act, M, N, K, x_pitch, w_pitch, residual_pitch, out_pitch)) return s;
-    return linear_i8_valu(a, out_type, reinterpret_cast<hipStream_t>(stream));
+    const int64_t tiles = (int64_t)ceil_div(M, kI8vT) * ((N - 1) / kI8vT + 1);
+    if (!launch_holds((double)tiles, 256)) return HB_ERR_UNSUPPORTED;
+    const auto st = reinterpret_cast<hipStream_t>(stream);
+    if (out_type == HB_F32) hipLaunchKernelGGL(linear_i8_valu_kernel<float>, dim3((unsigned)tiles), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(linear_i8_valu_kernel<half_t>, dim3((unsigned)tiles), dim3(256), 0, st, a);
+    return launch_status();
 }
 
 extern "C" hb_status hb_linear_i8(const int8_t* x, const int8_t* w, const float* x_scale, const float* w_scale, const hb_half* bias, const void* residual,
                                   void* out, hb_type out_type, hb_act act, int M, int N, int K, int64_t x_pitch, int64_t w_pitch,
                                   int64_t residual_pitch, int64_t out_pitch, void* workspace, size_t workspace_bytes, hb_stream stream) {
     using namespace hb;
-    (void)workspace;
-    (void)workspace_bytes;
-    LinearI8Args a;
+    LinearArgs<LinI8> a;
     if (hb_status s = linear_i8_prepare(a, x, w, x_scale, w_scale, bias, residual, out, out_type, act, M, N, K, x_pitch, w_pitch, residual_pitch, out_pitch)) return s;
-    return linear_i8_valu(a, out_type, reinterpret_cast<hipStream_t>(stream));
+    const auto st = reinterpret_cast<hipStream_t>(stream);
+    return out_type == HB_F32 ? linear_call<LinI8, float>(a, workspace, workspace_bytes, st) : linear_call<LinI8, half_t>(a, workspace, workspace_bytes, st);
 }

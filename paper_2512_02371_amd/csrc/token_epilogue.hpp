@@ -33,16 +33,16 @@ __device__ __forceinline__ float linear_act(float v, int act) {
 // `count` of V adjacent elements, at any address that their type allows.  Stores are streaming, whole lines of a row at a time, which is for what
 // they would push out of the caches: 100000 x 200 fp32, K 96, with a residual 48 -> 38 us, but 23 -> 33 without one; 2^20 x 64, K 64 with a residual
 // 83.8 -> 82.5; 8192 x 8192, K 2048 with gelu_tanh 245 -> 243, without 234 -> 238; smaller outputs within 5 %.
-template <int V, class T>
-__device__ __forceinline__ void lin_load(float (&v)[V], const T* from, int count) {
+template <int V, class S, class T>
+__device__ __forceinline__ void lin_load(S (&v)[V], const T* from, int count) {
     typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
     if (count >= V) {
         const vec q = *reinterpret_cast<const vec*>(from);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)q[i];
+        for (int i = 0; i < V; ++i) v[i] = (S)q[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = i < count ? (float)from[i] : 0.f;
+        for (int i = 0; i < V; ++i) v[i] = i < count ? (S)from[i] : (S)0;
     }
 }
 template <int V, class T>

@@ -3,6 +3,7 @@ functions against closed forms and loops over their definitions."""
 import ctypes
 import math
 import os
+import re
 from fractions import Fraction
 
 import numpy as np
@@ -21,6 +22,17 @@ def lib():
         import __graft_entry__
         __graft_entry__.build()
     return hb.load()
+
+
+def test_the_integer_product_has_one_wrapper():
+    """One shape, in one header: what test_matrix_builtins_appear_only_in_the_wrappers asks of the floating-point products."""
+    package = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2512_02371_amd")
+    assert os.listdir(os.path.join(package, "wrappers")) == ["mfma_i8.hpp"]
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(package, "wrappers", "mfma_i8.hpp")).read())
+    assert re.findall(r"__builtin_amdgcn_\w+", text) == ["__builtin_amdgcn_mfma_i32_16x16x64_i8"] and "asm" not in text
+    for name in os.listdir(os.path.join(package, "csrc")):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(package, "csrc", name)).read())
+        assert ("mfma16x16x64i8" in text) == (name == "linear_tiles.hpp"), name
 
 
 def test_group_norm_arguments(lib):
