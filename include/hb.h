@@ -484,7 +484,7 @@ hb_status hb_group_norm(const void *x, hb_type x_type, const hb_half *weight_or_
  *     scale[m] = max_k |x[m][k]| / 127,   q[m][k] = round(127 x[m][k] / max_k |x[m][k]|)   (ties to even)
  * The integers are those of the exact quotients, -127 .. 127; the scale is the fp32 number nearest to its quotient.  A row of zeros has scale 0 and zeros, a row with a NaN or
  * an infinity scale NaN and zeros.  x: M x K fp16, q: M x K int8, scale: M fp32.  M, K >= 1; pitches in elements, >= K (that of a single row has no
- * meaning); M less than 2^24 (HB_ERR_UNSUPPORTED beyond).  Base pointers need the alignment of their elements; fastest with 16-byte aligned
+ * meaning); M less than 2^24, K at most 2^31 - 2^17 (HB_ERR_UNSUPPORTED beyond).  Base pointers need the alignment of their elements; fastest with 16-byte aligned
  * rows of x and 8-byte aligned rows of q.
  */
 hb_status hb_quantize_rows(const hb_half *x, int8_t *q, float *scale, int M, int K, int64_t x_pitch, int64_t q_pitch, hb_stream stream);

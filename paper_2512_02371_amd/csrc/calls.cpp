@@ -22,7 +22,7 @@ PyObject* g_error = nullptr;                  // hb.HbError
 PyTypeObject* g_ndarray = nullptr;
 bool g_forked = false;                        // a child of fork() cannot use its parent's device: hb.py lets torch say so
 
-#define HB_CALLS(X) X(hb_fir1d) X(hb_conv2d) X(hb_down2) X(hb_up2) X(hb_sepblur) X(hb_sat2d) X(hb_conv3x3) X(hb_pyr_level) X(hb_resize) X(hb_iir2) X(hb_dct_denoise) X(hb_linear) X(hb_rope_axes) X(hb_attention)
+#define HB_CALLS(X) X(hb_fir1d) X(hb_conv2d) X(hb_down2) X(hb_up2) X(hb_sepblur) X(hb_sat2d) X(hb_conv3x3) X(hb_pyr_level) X(hb_resize) X(hb_iir2) X(hb_dct_denoise) X(hb_linear) X(hb_rope_axes) X(hb_attention) X(hb_group_norm) X(hb_quantize_rows) X(hb_linear_i8)
 struct Library {
 #define HB_POINTER(f) decltype(&::f) f = nullptr;
     HB_CALLS(HB_POINTER)
@@ -392,6 +392,105 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// On the current device, where the launch goes; hb.py says so where they are not.
+bool here(std::initializer_list<PyObject*> tensors) {
+    const auto now = c10::hip::current_device();
+    for (PyObject* o : tensors)
+        if (o != Py_None && THPVariable_Unpack(o).device().index() != now) return false;
+    return true;
+}
+// N x P x C or N x H x W x C, the channels adjacent and the pixels at one distance.
+struct Pixels {
+    void* p;
+    int n[3];
+    int64_t image, pixel;
+    hb_type type;
+};
+bool pixels(PyObject* o, Pixels& r) {
+    const at::Tensor* t = plain(o);
+    if (!t || (t->scalar_type() != at::kHalf && t->scalar_type() != at::kFloat)) return false;
+    const auto n = t->sizes(), s = t->strides();
+    const int64_t dims = t->dim();
+    if ((dims != 3 && dims != 4) || s[dims - 1] != 1) return false;
+    const int64_t all = dims == 3 ? n[1] : n[1] <= kMostInt && n[2] <= kMostInt ? n[1] * n[2] : kMostInt + 1;
+    if (n[0] > kMostInt || all > kMostInt || n[dims - 1] > kMostInt) return false;
+    r.pixel = s[dims - 2];
+    if (dims == 4 && n[1] != 1) {
+        if (n[2] == 1) r.pixel = s[1];
+        else if (s[1] != n[2] * r.pixel) return false;
+    }
+    r.p = t->data_ptr();
+    r.n[0] = (int)n[0], r.n[1] = (int)all, r.n[2] = (int)n[dims - 1];
+    r.image = s[0];
+    r.type = t->scalar_type() == at::kFloat ? HB_F32 : HB_F16;
+    return true;
+}
+// `n` adjacent values of a type, or, where there may be none, none.
+template <class T>
+bool values(PyObject* o, at::ScalarType type, int64_t n, bool none, const T*& p) {
+    p = nullptr;
+    if (none && o == Py_None) return true;
+    const at::Tensor* t = plain(o);
+    if (!t || t->scalar_type() != type || t->dim() != 1 || t->size(0) != n || !t->is_contiguous()) return false;
+    p = static_cast<const T*>(t->data_ptr());
+    return true;
+}
+
+PyObject* group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<8>(n, [&]() -> PyObject* {
+        Pixels x, o;
+        int groups;
+        const hb_half *weight, *bias;
+        float eps;
+        hb_act act;
+        void* ws;
+        size_t size;
+        if (!pixels(a[0], x) || !pixels(a[1], o) || THPVariable_Unpack(a[0]).sizes() != THPVariable_Unpack(a[1]).sizes() || !integer(a[2], groups) ||
+            !values(a[3], at::kHalf, x.n[2], true, weight) || !values(a[4], at::kHalf, x.n[2], true, bias) || !real(a[5], eps) || !activation(a[6], act) ||
+            !scratch(a[7], ws, size) || !here({a[0], a[1], a[3], a[4], a[7]})) Py_RETURN_FALSE;
+        return made("hb_group_norm", [&](hb_stream st) {
+            return g_lib.hb_group_norm(x.p, x.type, weight, bias, o.p, o.type, act, eps, x.n[0], x.n[1], x.n[2], groups, x.image, x.pixel, o.image, o.pixel, ws, size, st);
+        });
+    });
+}
+
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<3>(n, [&]() -> PyObject* {
+        Image x, q;
+        const float* scale;
+        if (!image(a[0], at::kHalf, 2, x) || !image(a[1], at::kChar, 2, q) || x.h != q.h || x.w != q.w || !values(a[2], at::kFloat, x.h, false, scale) ||
+            !here({a[0], a[1], a[2]})) Py_RETURN_FALSE;
+        return made("hb_quantize_rows", [&](hb_stream st) {
+            return g_lib.hb_quantize_rows(h(x.p), static_cast<int8_t*>(q.p), const_cast<float*>(scale), x.h, x.w, x.pitch, q.pitch, st);
+        });
+    });
+}
+
+PyObject* linear_i8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded<9>(n, [&]() -> PyObject* {
+        Image x, w, o, r{};
+        const at::Tensor* out = plain(a[4]);
+        if (!out || (out->scalar_type() != at::kHalf && out->scalar_type() != at::kFloat)) Py_RETURN_FALSE;
+        const at::ScalarType type = out->scalar_type();
+        const float *xs, *wsc;
+        const hb_half* bias;
+        void* ws;
+        size_t size;
+        hb_act act;
+        if (!image(a[0], at::kChar, 2, x) || !image(a[1], at::kChar, 2, w) || !values(a[2], at::kFloat, x.h, false, xs) || !values(a[3], at::kFloat, w.h, false, wsc) ||
+            !image(a[4], type, 2, o) || x.w != w.w || o.h != x.h || o.w != w.h || !scratch(a[5], ws, size) || !values(a[6], at::kHalf, w.h, true, bias) ||
+            !activation(a[8], act)) Py_RETURN_FALSE;
+        if (a[7] != Py_None && (!image(a[7], type, 2, r) || r.h != o.h || r.w != o.w)) Py_RETURN_FALSE;
+        if (!here({a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7]})) Py_RETURN_FALSE;
+        if (x.h == 1) x.pitch = x.w, o.pitch = r.pitch = o.w;                 // the pitch of a single row has no meaning, and torch gives any
+        if (w.h == 1) w.pitch = w.w;
+        return made("hb_linear_i8", [&](hb_stream st) {
+            return g_lib.hb_linear_i8(static_cast<const int8_t*>(x.p), static_cast<const int8_t*>(w.p), xs, wsc, bias, r.p, o.p, type == at::kFloat ? HB_F32 : HB_F16, act,
+                                      x.h, w.h, x.w, x.pitch, w.pitch, r.pitch, o.pitch, ws, size, st);
+        });
+    });
+}
+
 // bind({entry point: address}, error class): what load() found.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 2 || !PyDict_Check(a[0])) {
@@ -420,7 +519,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define HB_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HB_METHOD(bind), HB_METHOD(fir1d), HB_METHOD(conv2d), HB_METHOD(down2), HB_METHOD(up2), HB_METHOD(sepblur), HB_METHOD(sat2d),
                          HB_METHOD(conv3x3), HB_METHOD(pyr_level), HB_METHOD(resize), HB_METHOD(iir2), HB_METHOD(dct_denoise), HB_METHOD(linear),
-                         HB_METHOD(rope_axes), HB_METHOD(attention), {nullptr, nullptr, 0, nullptr}};
+                         HB_METHOD(rope_axes), HB_METHOD(attention), HB_METHOD(group_norm), HB_METHOD(quantize_rows), HB_METHOD(linear_i8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

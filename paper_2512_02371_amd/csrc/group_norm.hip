@@ -8,6 +8,18 @@
 
 namespace hb {
 
+// Division by a number that the host knows: the product with floor(2^32 / d) is the quotient or one less.
+struct NormDiv {
+    uint32_t d, m;
+    __device__ __forceinline__ uint32_t by(uint32_t a, uint32_t& rest) const {
+        uint32_t q = __umulhi(a, m);
+        rest = a - q * d;
+        if (rest >= d) rest -= d, ++q;
+        return q;
+    }
+};
+static NormDiv norm_div(int d) { return {(uint32_t)d, d == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / d)}; }
+
 struct NormArgs {
     const void* x;
     void* out;
@@ -20,9 +32,14 @@ struct NormArgs {
     int N, P, C, G, D;
     int64_t x_image, x_row, out_image, out_row;
     int pixels, groups, images, width, rows, blocks, passes, chunk, chunks;    // as in NormPlan
+    int apply_chunk, apply_chunks;
+    int log_pixels;
     int lanes_row;             // rows side by side in a workgroup
     int log_lanes;             // lanes that add up a group: 2^this
-    int step_d, step_r;        // these lanes in entries of a group's row, and in rows
+    int size;                  // most entries of a group in a row
+    int step_d, step_r;        // these lanes in entries and rows
+    NormDiv by_all, by_width, by_size, by_D, by_blocks, by_chunks, by_apply_chunks;     // images * width, ...
+    double inverse_P;
     int stream;                // results past the caches
 };
 
@@ -34,7 +51,7 @@ struct NormVec {
 
 // Where a lane stands.
 struct NormLane {
-    int row, column;           // of the workgroup; columns are vectors
+    int row;                   // of the workgroup
     int image, at;             // image of the workgroup, first channel in the row of its block
     bool there;
     int valid, valid_last;     // elements of its vector in a row, and in the image's last row
@@ -42,11 +59,10 @@ struct NormLane {
 template <int V>
 __device__ __forceinline__ NormLane norm_lane(const NormArgs& p, int first_image, int block) {
     NormLane l;
-    const int all = p.images * p.width;
-    l.row = threadIdx.x / (unsigned)all;
-    l.column = threadIdx.x - l.row * all;
-    l.image = l.column / (unsigned)p.width;
-    l.at = (l.column - l.image * p.width) * V;
+    uint32_t column, at;
+    l.row = p.by_all.by(threadIdx.x, column);
+    l.image = p.by_width.by(column, at);
+    l.at = at * V;
     const int channels = min(p.groups, p.G - block * p.groups) * p.D, length = p.pixels * channels;
     l.there = l.row < p.lanes_row && first_image + l.image < p.N && l.at < length;
     l.valid = max(0, min(V, length - l.at));
@@ -66,28 +82,55 @@ __device__ __forceinline__ typename NormVec<X>::type norm_load(const X* from, in
     return r;
 }
 
-// The entries of group q of the workgroup that belong to one of the lanes that add it up: f(index).  An entry is an element of a lane, or, where a vector
-// is of one group (ONE), a lane; entries of a row are adjacent, a group's are D (or D / V) of them, once for each pixel of a row.
-template <int V, bool ONE, class F>
+// What a lane leaves of its V elements for the sums of their groups: an entry for all of them where a vector is of one group (kNormOne), two where groups are as wide as a
+// vector or wider (kNormTwo: what belongs to the first element's group, and what to the next), else one for each.
+enum NormKind { kNormOne, kNormTwo, kNormEach };
+template <NormKind KIND, int V>
+constexpr int kNormEntries = KIND == kNormOne ? 1 : KIND == kNormTwo ? 2 : V;
+
+// f(index, whether there is one) for the entries of group q of the workgroup that belong to one of the lanes that add it up.  A row's entries are adjacent; a group has p.size of
+// them at most, once for each pixel of a row.
+template <int V, NormKind KIND, class F>
 __device__ __forceinline__ void norm_entries(const NormArgs& p, int q, int lane, F f) {
-    const int per = ONE ? 1 : V, size = ONE ? p.D / V : p.D, length = p.images * p.width * per;
-    const int image = q / (unsigned)p.groups, first = image * p.width * per + (q - image * p.groups) * size;
-    int r = lane / (unsigned)size, d = lane - r * size;
-    if (p.pixels == 1) {
-        for (; r < p.lanes_row;) {
-            f(r * length + first + d);
-            d += p.step_d;
-            r += p.step_r + (d >= size);
-            d -= d >= size ? size : 0;
+    constexpr int E = kNormEntries<KIND, V>;
+    const int image = p.images > 1 ? q / (unsigned)p.groups : 0, first = (q - image * p.groups) * p.D;
+    const int length = p.images * p.width * E, base = image * p.width * E;
+    uint32_t begin;
+    int r = p.by_size.by(lane, begin), d = begin;
+    const int total = (p.lanes_row << p.log_pixels) * p.size, lanes = 1 << p.log_lanes;
+#pragma unroll 4
+    for (int left = (total - lane + lanes - 1) >> p.log_lanes; left > 0; --left) {
+        const int row = r >> p.log_pixels, from = first + (r - (row << p.log_pixels)) * p.C;         // the group's first element in the row
+        bool there = true;
+        int e;
+        if (KIND == kNormTwo) {
+            const int vector = from / V + d;
+            there = vector * V < from + p.D;
+            e = there ? row * length + base + 2 * vector + (vector * V < from) : 0;
+        } else {
+            e = row * length + base + (KIND == kNormOne ? from / V : from) + d;
         }
+        f(e, there);
+        d += p.step_d;
+        r += p.step_r + (d >= p.size);
+        d -= d >= p.size ? p.size : 0;
+    }
+}
+// A lane's entries of V values; `cut`: how many belong to the first element's group.
+template <int V, NormKind KIND>
+__device__ __forceinline__ void norm_fold(const float (&v)[KIND == kNormOne ? 1 : V], int cut, float* to) {
+    if (KIND == kNormTwo) {
+        float a = 0.f, b = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            a += i < cut ? v[i] : 0.f;
+            b += i < cut ? 0.f : v[i];
+        }
+        to[0] = a;
+        to[1] = b;
     } else {
-        for (; r < p.lanes_row * p.pixels;) {
-            const int row = r / (unsigned)p.pixels;
-            f(row * length + (r - row * p.pixels) * p.C + first + d);
-            d += p.step_d;
-            r += p.step_r + (d >= size);
-            d -= d >= size ? size : 0;
-        }
+#pragma unroll
+        for (int i = 0; i < kNormEntries<KIND, V>; ++i) to[i] = v[i];
     }
 }
 // Sum over the lanes that share a group, the same in all of them.
@@ -96,11 +139,13 @@ __device__ __forceinline__ float norm_lanes_sum(float v, int log_lanes) {
     return v;
 }
 
-// The groups of a lane's elements in the workgroup, and their channels in the image.
+// The groups of a lane's elements in the workgroup, their channels in the image, and how many are of the first one's group.
 template <int V, bool ONE>
-__device__ __forceinline__ void norm_channels(const NormArgs& p, const NormLane& l, int block, int (&group)[ONE ? 1 : V], uint32_t (&channel)[V]) {
-    int c = p.pixels > 1 ? l.at % (unsigned)p.C : l.at, g = c / (unsigned)p.D, d = c - g * p.D;
-    const int own = min(p.groups, p.G - block * p.groups), first = block * p.groups * p.D;
+__device__ __forceinline__ int norm_channels(const NormArgs& p, const NormLane& l, int block, int (&group)[ONE ? 1 : V], uint32_t (&channel)[V]) {
+    int c = p.pixels > 1 ? l.at % (unsigned)p.C : l.at;
+    uint32_t in;
+    int g = p.by_D.by(c, in), d = in;
+    const int own = min(p.groups, p.G - block * p.groups), first = block * p.groups * p.D, cut = min(V, p.D - d);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         channel[i] = first + min(c, own * p.D - 1);
@@ -109,6 +154,7 @@ __device__ __forceinline__ void norm_channels(const NormArgs& p, const NormLane&
         if (++d == p.D) d = 0, ++g;
         if (p.pixels > 1 && c == p.C) c = 0, g = 0, d = 0;
     }
+    return cut;
 }
 
 // The weights or biases of a lane's channels; `none` where there are none.
@@ -162,166 +208,204 @@ __device__ __forceinline__ void norm_with(int act, F f) {
 // ---------------------------------------------------------------------------
 // Groups whose pixels fit the registers of a workgroup: x is read once, the mean and then the squares of the differences from it are added up in registers, over
 // the lanes through LDS, and the results leave.
-template <class X, class O, int SLOTS, bool FULL, bool ONE>
+template <class X, class O, int SLOTS, bool FULL, NormKind KIND>
 __global__ void __launch_bounds__(kNormThreads) norm_slab_kernel(NormArgs p) {
     using vec = typename NormVec<X>::type;
-    constexpr int V = NormVec<X>::V, E = ONE ? 1 : V;
+    constexpr int V = NormVec<X>::V, E = kNormEntries<KIND, V>;
+    constexpr bool ONE = KIND == kNormOne;
+    constexpr int S = ONE ? 1 : V;                        // sums of a lane
     extern __shared__ float s_norm[];
     const int nT = blockDim.x, nG = p.images * p.groups;
     float *const s_a = s_norm, *const s_b = s_a + nT * E, *const s_mean = s_b + nT * E, *const s_rstd = s_mean + nG;
-    const int id = xcd_blocked(blockIdx.x, gridDim.x, 8), block = id % p.blocks, first_image = id / p.blocks * p.images;
+    uint32_t block_;
+    const int first_image = (int)p.by_blocks.by(xcd_blocked(blockIdx.x, gridDim.x, 8), block_) * p.images, block = block_;
     const NormLane l = norm_lane<V>(p, first_image, block);
     const int n = min(first_image + l.image, p.N - 1);
     const int offset = block * p.groups * p.D + (l.there ? l.at : 0);
     const X* const x = static_cast<const X*>(p.x) + n * p.x_image + offset;
 
+    // Slot i of a lane is its row l.row + i * lanes_row: all there but for the last slot, and the image's last row is in that.
+    const int last_row = l.row + (p.passes - 1) * p.lanes_row;
+    const int valid = l.there ? l.valid : 0, last = !l.there || last_row >= p.rows ? 0 : last_row == p.rows - 1 ? l.valid_last : l.valid;
     vec held[SLOTS];
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i)
-        if (i < p.passes) {
-            const int row = min(l.row + i * p.lanes_row, p.rows - 1);
-            held[i] = norm_load<X, FULL>(x + row * p.x_row, !l.there ? 0 : row == p.rows - 1 ? l.valid_last : l.valid);
-        }
-    int group[E];
-    uint32_t channel[V];
-    norm_channels<V, ONE>(p, l, block, group, channel);
-    const auto weight = norm_per_channel<V>(p.weight, 1.f, channel, p.pixels == 1 && l.valid == V), bias = norm_per_channel<V>(p.bias, 0.f, channel, p.pixels == 1 && l.valid == V);
-    // rows of this lane, and what of its vector counts in each
-    auto rows = [&](auto f) HB_INLINE {
+    {
+        const X* from = x + (int64_t)min(l.row, p.rows - 1) * p.x_row;
+        const int64_t step = (int64_t)p.lanes_row * p.x_row;
 #pragma unroll
         for (int i = 0; i < SLOTS; ++i)
             if (i < p.passes) {
-                const int row = l.row + i * p.lanes_row;
-                if (l.there && row < p.rows) f(held[i], row, FULL ? V : row == p.rows - 1 ? l.valid_last : l.valid);
+                if (i > 0) from = i == p.passes - 1 ? x + (int64_t)min(last_row, p.rows - 1) * p.x_row : from + step;
+                held[i] = norm_load<X, FULL>(from, i == p.passes - 1 ? last : valid);
+            }
+    }
+    int group[S];
+    uint32_t channel[V];
+    const int cut = norm_channels<V, ONE>(p, l, block, group, channel);
+    const auto weight = norm_per_channel<V>(p.weight, 1.f, channel, p.pixels == 1 && l.valid == V), bias = norm_per_channel<V>(p.bias, 0.f, channel, p.pixels == 1 && l.valid == V);
+    // f(vector, its slot, what of it counts) for each of them
+    auto rows = [&](auto f) HB_INLINE {
+        int some = valid, end = last, passes = p.passes;
+        asm volatile("" : "+v"(some), "+v"(end), "+s"(passes));              // or what each slot compares would be kept from one use to the next, in registers that there are not
+        tk_for<SLOTS>([&](auto index) HB_INLINE {
+            constexpr int i = decltype(index)::value;
+            if (i < passes) {
+                const int counts = i == passes - 1 ? end : some;
+                if (counts > 0) f(held[i], i, FULL ? V : counts);
                 __builtin_amdgcn_sched_barrier(0);        // one vector's values at a time: several would not fit the registers
             }
+        });
     };
     const float count = (float)p.P * (float)p.D;
     const int lane = threadIdx.x & ((1 << p.log_lanes) - 1);
 
-    float a[E] = {}, b[E] = {};
-    rows([&](const vec& v, int, int) HB_INLINE {          // what is not valid is zero
+    // About the mean of the first vectors, while the others are on their way.
+    float a[S] = {}, b[S] = {};
+    if ((p.passes == 1 ? last : valid) > 0) {             // what is not valid is zero
 #pragma unroll
-        for (int i = 0; i < V; ++i) a[ONE ? 0 : i] += (float)v[i];
-    });
-#pragma unroll
-    for (int i = 0; i < E; ++i) s_a[threadIdx.x * E + i] = a[i];
-    __syncthreads();
+        for (int i = 0; i < V; ++i) a[ONE ? 0 : i] += (float)held[0][i];
+    }
+    norm_fold<V, KIND>(a, cut, s_a + threadIdx.x * E);
+    lds_barrier();
+    const float first = p.passes == 1 ? count : (float)p.lanes_row * (float)p.pixels * (float)p.D;
     for (int q = threadIdx.x >> p.log_lanes; q < nG; q += nT >> p.log_lanes) {
         float sum = 0.f;
-        norm_entries<V, ONE>(p, q, lane, [&](int e) HB_INLINE { sum += s_a[e]; });
+        norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE { sum += there ? s_a[e] : 0.f; });
         sum = norm_lanes_sum(sum, p.log_lanes);
-        if (lane == 0) s_mean[q] = sum / count;
+        if (lane == 0) s_mean[q] = sum / first;
     }
-    __syncthreads();
-    float mean[E];
+    lds_barrier();
+    // Twice only where the first vectors say so little of the others that the squares about them have lost digits: more than four deviations from the mean.
+    float mean[S];
+    for (int again = 0;; ++again) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) mean[i] = s_mean[group[i]], a[i] = 0.f;
-    rows([&](const vec& v, int, int valid) HB_INLINE {
+        for (int i = 0; i < SLOTS; ++i) asm volatile("" : "+v"(held[i]));    // or their conversions would be kept from turn to turn, in registers that there are not
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float d = i < valid ? (float)v[i] - mean[ONE ? 0 : i] : 0.f;
-            a[ONE ? 0 : i] += d;
-            b[ONE ? 0 : i] = fmaf(d, d, b[ONE ? 0 : i]);
-        }
-    });
+        for (int i = 0; i < S; ++i) mean[i] = s_mean[group[i]], a[i] = b[i] = 0.f;
+        rows([&](const vec& v, int, int valid) HB_INLINE {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        s_a[threadIdx.x * E + i] = a[i];
-        s_b[threadIdx.x * E + i] = b[i];
-    }
-    __syncthreads();
-    for (int q = threadIdx.x >> p.log_lanes; q < nG; q += nT >> p.log_lanes) {
-        float left = 0.f, squares = 0.f;
-        norm_entries<V, ONE>(p, q, lane, [&](int e) HB_INLINE {
-            left += s_a[e];
-            squares += s_b[e];
+            for (int i = 0; i < V; ++i) {
+                const float d = FULL || i < valid ? (float)v[i] - mean[ONE ? 0 : i] : 0.f;
+                a[ONE ? 0 : i] += d;
+                b[ONE ? 0 : i] = fmaf(d, d, b[ONE ? 0 : i]);
+            }
         });
-        left = norm_lanes_sum(left, p.log_lanes) / count;                    // what the rounded sum left of the mean
-        squares = norm_lanes_sum(squares, p.log_lanes) / count;
-        if (lane == 0) {
-            s_mean[q] += left;
-            s_rstd[q] = 1.f / sqrtf(fmaxf(squares - left * left, 0.f) + p.eps);
+        norm_fold<V, KIND>(a, cut, s_a + threadIdx.x * E);
+        norm_fold<V, KIND>(b, cut, s_b + threadIdx.x * E);
+        __syncthreads();
+        int far = 0;
+        for (int q = threadIdx.x >> p.log_lanes; q < nG; q += nT >> p.log_lanes) {
+            float left = 0.f, squares = 0.f;
+            norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE {
+                left += there ? s_a[e] : 0.f;
+                squares += there ? s_b[e] : 0.f;
+            });
+            left = norm_lanes_sum(left, p.log_lanes) / count;
+            squares = norm_lanes_sum(squares, p.log_lanes) / count;
+            const float var = fmaxf(squares - left * left, 0.f);
+            far |= left * left > 16.f * var;
+            if (lane == 0) {
+                s_mean[q] += left;
+                s_rstd[q] = 1.f / sqrtf(var + p.eps);
+            }
         }
+        if (p.passes == 1 || again == 1) {
+            __syncthreads();
+            break;
+        }
+        if (!__syncthreads_or(far)) break;
     }
-    __syncthreads();
     float scale[V];
 #pragma unroll
-    for (int i = 0; i < E; ++i) mean[i] = s_mean[group[i]];
+    for (int i = 0; i < S; ++i) mean[i] = s_mean[group[i]];
 #pragma unroll
     for (int i = 0; i < V; ++i) scale[i] = s_rstd[group[ONE ? 0 : i]] * (float)weight[i];
-    O* const out = static_cast<O*>(p.out) + n * p.out_image + offset;
+    O* out = static_cast<O*>(p.out) + n * p.out_image + offset + l.row * p.out_row;
+    const int64_t step = (int64_t)p.lanes_row * p.out_row;
     norm_with(p.act, [&](auto act) HB_INLINE {
-        rows([&](const vec& v, int row, int valid) HB_INLINE {
+        rows([&](const vec& v, int slot, int valid) HB_INLINE {
             float y[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = act(fmaf((float)v[i] - mean[ONE ? 0 : i], scale[i], (float)bias[i]));
-            norm_store<O, V>(out + row * p.out_row, y, FULL ? V : valid, p.stream);
+            norm_store<O, V>(out + slot * step, y, FULL ? V : valid, p.stream);
         });
     });
 }
 
 // ---------------------------------------------------------------------------
-// Larger groups.  A workgroup reads a chunk of rows and leaves mean and sum of squared differences of each of its groups; a wave joins the chunks of a group; and
-// the rows are read once more.  Every joining takes the means first and the squares about the joint mean, so that no digits are lost where a mean is far from zero.
-template <class X, bool FULL, bool ONE>
+// Larger groups.  A workgroup reads a chunk of rows and leaves mean and sum of squared differences of each of its groups; the chunks of a group are joined, by a wave of a launch
+// of its own or, where they are few, by every workgroup of the next; and the rows are read once more.  Every joining takes the means first and the squares about the joint
+// mean, so that no digits are lost where a mean is far from zero.
+
+// U rows of a lane from `row` on, as many as there are before `end`: their vectors, and how many.
+template <class X, bool FULL, int U>
+__device__ __forceinline__ int norm_batch(const NormArgs& p, const X* x, int row, int end, const NormLane& l, typename NormVec<X>::type (&v)[U]) {
+    int have = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int at = row + u * p.lanes_row;
+        have += at < end;
+        const int from = min(at, end - 1);                // what is not there is loaded from what is
+        v[u] = norm_load<X, FULL>(x + (int64_t)from * p.x_row, from == p.rows - 1 ? l.valid_last : l.valid);
+    }
+    return have;
+}
+
+template <class X, bool FULL, NormKind KIND>
 __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs p) {
     using vec = typename NormVec<X>::type;
-    constexpr int V = NormVec<X>::V, E = ONE ? 1 : V, U = kNormBatch;
+    constexpr int V = NormVec<X>::V, E = kNormEntries<KIND, V>, U = FULL ? kNormBatch : kNormBatch / 2;
+    constexpr bool ONE = KIND == kNormOne;
     extern __shared__ float s_norm[];
     const int nT = blockDim.x;
     float *const s_count = s_norm, *const s_mean = s_count + nT * E, *const s_squares = s_mean + nT * E;
-    const int chunk = blockIdx.x % (unsigned)p.chunks, rest = blockIdx.x / (unsigned)p.chunks, block = rest % p.blocks, n = rest / p.blocks;
+    uint32_t chunk_, block_;
+    const int n = p.by_blocks.by(p.by_chunks.by(blockIdx.x, chunk_), block_), block = block_, chunk = chunk_;
     const NormLane l = norm_lane<V>(p, n, block);
     const X* const x = static_cast<const X*>(p.x) + n * p.x_image + block * p.groups * p.D + (l.there ? l.at : 0);
     // a last row that is shorter than the others comes by itself
-    const bool ragged = !FULL && (int64_t)p.rows * p.pixels > p.P;
+    const bool ragged = !FULL && ((int64_t)p.rows << p.log_pixels) > p.P;
     const int begin = chunk * p.chunk, end = min(begin + p.chunk, p.rows - ragged);
     float count = 0.f, mean[V] = {}, squares[V] = {};
-    auto join = [&](float more, const float (&m)[V], const float (&s)[V]) HB_INLINE {
-        const float f = more / (count + more), g = count * f;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float d = m[i] - mean[i];
-            mean[i] = fmaf(d, f, mean[i]);
-            squares[i] += fmaf(d * d, g, s[i]);
-        }
-        count += more;
-    };
     float extra[V] = {};       // elements of the short row
     if (l.there) {
         int row = begin + l.row;
-        const X* from = x + row * p.x_row;
-        for (; row + (U - 1) * p.lanes_row < end; row += U * p.lanes_row) {
+        if (row < end) {
             vec v[U];
+            int have = norm_batch<X, FULL, U>(p, x, row, end, l, v);
+            for (;;) {
+                vec next[U];
+                int have_next = 0;
+                row += U * p.lanes_row;
+                if (row < end) have_next = norm_batch<X, FULL, U>(p, x, row, end, l, next);
+                const float more = (float)have, inverse = 1.f / more, f = more / (count + more), g = count * f;
+                auto join = [&](auto whole) HB_INLINE {
+                    constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = norm_load<X, FULL>(from + (int64_t)(u * p.lanes_row) * p.x_row, l.valid);
-            from += (int64_t)(U * p.lanes_row) * p.x_row;
-            float m[V], s[V];
+                    for (int i = 0; i < V; ++i) {
+                        float m = 0.f, s = 0.f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                m[i] = 0.f;
+                        for (int u = 0; u < U; ++u) m += WHOLE || u < have ? (float)v[u][i] : 0.f;
+                        m *= inverse;
 #pragma unroll
-                for (int u = 0; u < U; ++u) m[i] += (float)v[u][i];
-                m[i] *= 1.f / U;
-                s[i] = 0.f;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const float d = (float)v[u][i] - m[i];
-                    s[i] = fmaf(d, d, s[i]);
-                }
+                        for (int u = 0; u < U; ++u) {
+                            const float d = WHOLE || u < have ? (float)v[u][i] - m : 0.f;
+                            s = fmaf(d, d, s);
+                        }
+                        const float d = m - mean[i];
+                        mean[i] = fmaf(d, f, mean[i]);
+                        squares[i] += fmaf(d * d, g, s);
+                    }
+                };
+                if (have == U) join(TkInt<1>{});
+                else join(TkInt<0>{});
+                count += more;
+                if (have_next == 0) break;
+                have = have_next;
+                tk_for<U>([&](auto u) HB_INLINE { v[decltype(u)::value] = next[decltype(u)::value]; });
             }
-            join((float)U, m, s);
         }
-        for (; row < end; row += p.lanes_row) {
-            const vec v = norm_load<X, FULL>(x + row * p.x_row, l.valid);
-            float m[V], s[V] = {};
-#pragma unroll
-            for (int i = 0; i < V; ++i) m[i] = (float)v[i];
-            join(1.f, m, s);
-        }
-        if (!FULL && ragged && row == p.rows - 1 && row < begin + p.chunk) {
-            const vec v = norm_load<X, FULL>(x + row * p.x_row, l.valid_last);
+        if (!FULL && ragged && chunk == p.chunks - 1 && (p.rows - 1 - begin) % p.lanes_row == l.row) {
+            const vec v = norm_load<X, FULL>(x + (int64_t)(p.rows - 1) * p.x_row, l.valid_last);
             const float f = 1.f / (count + 1.f);
 #pragma unroll
             for (int i = 0; i < V; ++i)
@@ -333,45 +417,60 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs p) {
                 }
         }
     }
-    if (ONE) {                                            // the lane's elements are of one group
-        float m = 0.f, left = 0.f, s = 0.f;
-#pragma unroll
-        for (int i = 0; i < V; ++i) m += mean[i];
-        m *= 1.f / V;
+    // elements from `from` on, `n` of them, as one entry
+    int group[ONE ? 1 : V];
+    uint32_t channel[V];
+    const int cut = norm_channels<V, ONE>(p, l, block, group, channel);
+    auto entry = [&](int e, auto in) HB_INLINE {
+        float c = 0.f, m = 0.f, left = 0.f, s = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float d = mean[i] - m;
-            left += d;
-            s += fmaf(d * d, count, squares[i]);
+            const float k = in(i) ? count + extra[i] : 0.f;
+            c += k;
+            m = fmaf(k, mean[i], m);
         }
-        left *= 1.f / V;
-        s_count[threadIdx.x] = V * count;
-        s_mean[threadIdx.x] = m + left;
-        s_squares[threadIdx.x] = fmaxf(fmaf(-V * count * left, left, s), 0.f);
-        if (s != s) s_squares[threadIdx.x] = s;
+        const float inverse = c > 0.f ? 1.f / c : 0.f;
+        m *= inverse;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float k = in(i) ? count + extra[i] : 0.f, d = mean[i] - m;
+            left = fmaf(k, d, left);
+            s += in(i) ? fmaf(k * d, d, squares[i]) : 0.f;
+        }
+        left *= inverse;
+        s_count[threadIdx.x * E + e] = c;
+        s_mean[threadIdx.x * E + e] = m + left;
+        s_squares[threadIdx.x * E + e] = fmaf(-c * left, left, s);
+    };
+    if (KIND == kNormOne) {
+        entry(0, [](int) HB_INLINE { return true; });
+    } else if (KIND == kNormTwo) {
+        entry(0, [&](int i) HB_INLINE { return i < cut; });
+        entry(1, [&](int i) HB_INLINE { return i >= cut; });
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            s_count[threadIdx.x * V + i] = count + extra[i];
-            s_mean[threadIdx.x * V + i] = mean[i];
-            s_squares[threadIdx.x * V + i] = squares[i];
+            s_count[threadIdx.x * E + i] = count + extra[i];
+            s_mean[threadIdx.x * E + i] = mean[i];
+            s_squares[threadIdx.x * E + i] = squares[i];
         }
     }
     __syncthreads();
     const int lane = threadIdx.x & ((1 << p.log_lanes) - 1);
     for (int q = threadIdx.x >> p.log_lanes; q < p.groups; q += nT >> p.log_lanes) {
         float c = 0.f, m = 0.f;
-        norm_entries<V, ONE>(p, q, lane, [&](int e) HB_INLINE {
-            c += s_count[e];
-            m = fmaf(s_count[e], s_mean[e], m);
+        norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE {
+            const float k = there ? s_count[e] : 0.f;
+            c += k;
+            m = fmaf(k, s_mean[e], m);
         });
         c = norm_lanes_sum(c, p.log_lanes);
         m = norm_lanes_sum(m, p.log_lanes) / c;
         float left = 0.f, s = 0.f;
-        norm_entries<V, ONE>(p, q, lane, [&](int e) HB_INLINE {
-            const float d = s_mean[e] - m, cd = s_count[e] * d;
+        norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE {
+            const float d = s_mean[e] - m, cd = there ? s_count[e] * d : 0.f;
             left += cd;
-            s += fmaf(cd, d, s_squares[e]);
+            s += there ? fmaf(cd, d, s_squares[e]) : 0.f;
         });
         left = norm_lanes_sum(left, p.log_lanes) / c;
         s = norm_lanes_sum(s, p.log_lanes);
@@ -380,98 +479,133 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs p) {
     }
 }
 
-// A wave per group of an image.  In 64 bits: nothing here is on the path of an element.
-__global__ void __launch_bounds__(64) norm_join_kernel(NormArgs p) {
-    const int64_t q = blockIdx.x;
-    const float2* parts = p.parts + q * p.chunks;
-    auto pixels = [&](int chunk) HB_INLINE {
-        const int64_t span = (int64_t)p.chunk * p.pixels, begin = chunk * span;
-        return (double)(begin + span < p.P ? span : p.P - begin);
-    };
-    auto all = [&](double v) HB_INLINE {
+// Mean and 1 / sqrt(var + eps) of a group from its chunks, at most kNormJoin of a lane's, by 2^log_lanes lanes; the same in all of them.  In 64 bits: nothing here is on
+// the path of an element.
+__device__ __forceinline__ float2 norm_join(const NormArgs& p, const float2* parts, int lane, int log_lanes) {
+    float2 part[kNormJoin];
+    int at[kNormJoin];
 #pragma unroll
-        for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
+    for (int i = 0; i < kNormJoin; ++i) {
+        at[i] = lane + (i << log_lanes);
+        part[i] = parts[min(at[i], p.chunks - 1)];
+    }
+    const int span = p.chunk << p.log_pixels;
+    const double most = (double)span, least = (double)(p.P - (int64_t)(p.chunks - 1) * span);      // pixels of a chunk, and of the last
+    auto pixels = [&](int i) HB_INLINE { return at[i] < p.chunks - 1 ? most : at[i] == p.chunks - 1 ? least : 0.0; };
+    auto all = [&](double v) HB_INLINE {
+        for (int m = 1 << log_lanes >> 1; m > 0; m >>= 1) v += __shfl_xor(v, m);
         return v;
     };
     double mean = 0.0, squares = 0.0;
-    for (int i = threadIdx.x; i < p.chunks; i += 64) mean += pixels(i) * (double)parts[i].x;
-    mean = all(mean) / (double)p.P;
-    for (int i = threadIdx.x; i < p.chunks; i += 64) {
-        const double d = (double)parts[i].x - mean;
-        squares += (double)parts[i].y + pixels(i) * p.D * d * d;
+#pragma unroll
+    for (int i = 0; i < kNormJoin; ++i) mean += pixels(i) * (double)part[i].x;
+    mean = all(mean) * p.inverse_P;
+#pragma unroll
+    for (int i = 0; i < kNormJoin; ++i) {
+        const double d = (double)part[i].x - mean;
+        squares += (at[i] < p.chunks ? (double)part[i].y : 0.0) + pixels(i) * p.D * d * d;
     }
-    squares = all(squares) / ((double)p.P * p.D);
-    if (threadIdx.x == 0) p.stats[q] = float2{(float)mean, 1.f / sqrtf((squares < 0.0 ? 0.f : (float)squares) + p.eps)};
+    squares = all(squares) * p.inverse_P / (float)p.D;
+    return float2{(float)mean, 1.f / sqrtf((squares < 0.0 ? 0.f : (float)squares) + p.eps)};
+}
+__global__ void __launch_bounds__(64) norm_join_kernel(NormArgs p) {
+    const int64_t q = blockIdx.x;
+    const float2 r = norm_join(p, p.parts + q * p.chunks, threadIdx.x, 6);
+    if (threadIdx.x == 0) p.stats[q] = r;
 }
 
-template <class X, class O, bool FULL, bool ONE>
+template <class X, class O, bool FULL, bool ONE, bool JOINED>
 __global__ void __launch_bounds__(kNormThreads) norm_apply_kernel(NormArgs p) {
     using vec = typename NormVec<X>::type;
-    constexpr int V = NormVec<X>::V, E = ONE ? 1 : V, U = kNormBatch;
-    const int chunk = blockIdx.x % (unsigned)p.chunks, rest = blockIdx.x / (unsigned)p.chunks, block = rest % p.blocks, n = rest / p.blocks;
+    constexpr int V = NormVec<X>::V, S = ONE ? 1 : V, U = kNormBatch / 2;
+    extern __shared__ float s_norm[];
+    uint32_t chunk_, block_;
+    const int n = p.by_blocks.by(p.by_apply_chunks.by(blockIdx.x, chunk_), block_), block = block_, chunk = chunk_;
     const NormLane l = norm_lane<V>(p, n, block);
-    if (!l.there) return;
-    const int offset = block * p.groups * p.D + l.at;
+    const int offset = block * p.groups * p.D + (l.there ? l.at : 0);
     const X* const x = static_cast<const X*>(p.x) + n * p.x_image + offset;
     O* const out = static_cast<O*>(p.out) + n * p.out_image + offset;
-    int group[E];
+    const int begin = chunk * p.apply_chunk, end = min(begin + p.apply_chunk, p.rows);
+    int row = begin + l.row, have = 0;
+    vec v[U];
+    if (l.there && row < end) have = norm_batch<X, FULL, U>(p, x, row, end, l, v);
+    int group[S];
     uint32_t channel[V];
     norm_channels<V, ONE>(p, l, block, group, channel);
-    float mean[E], scale[V], shift[V];
-    const float2* stats = p.stats + (int64_t)n * p.G + block * p.groups;
-#pragma unroll
-    for (int i = 0; i < E; ++i) mean[i] = stats[group[i]].x;
     const auto weight = norm_per_channel<V>(p.weight, 1.f, channel, p.pixels == 1 && l.valid == V), bias = norm_per_channel<V>(p.bias, 0.f, channel, p.pixels == 1 && l.valid == V);
+    float mean[S], scale[V];
+    if (JOINED) {
+        const float2* stats = p.stats + (int64_t)n * p.G + block * p.groups;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        scale[i] = stats[group[ONE ? 0 : i]].y * (float)weight[i];
-        shift[i] = (float)bias[i];
-    }
-    const int begin = chunk * p.chunk, end = min(begin + p.chunk, p.rows);
-    norm_with(p.act, [&](auto act) HB_INLINE {
-        auto store = [&](const vec& v, int row, int valid) HB_INLINE {
-            float y[V];
+        for (int i = 0; i < S; ++i) mean[i] = stats[group[i]].x;
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = act(fmaf((float)v[i] - mean[ONE ? 0 : i], scale[i], shift[i]));
-            norm_store<O, V>(out + row * p.out_row, y, valid, p.stream);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        auto valid = [&](int row) HB_INLINE { return FULL ? V : row == p.rows - 1 ? l.valid_last : l.valid; };
-        int row = begin + l.row;
-        for (; row + (U - 1) * p.lanes_row < end; row += U * p.lanes_row) {
-            vec v[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = norm_load<X, FULL>(x + (int64_t)(row + u * p.lanes_row) * p.x_row, valid(row + u * p.lanes_row));
-#pragma unroll
-            for (int u = 0; u < U; ++u) store(v[u], row + u * p.lanes_row, valid(row + u * p.lanes_row));
+        for (int i = 0; i < V; ++i) scale[i] = stats[group[ONE ? 0 : i]].y * (float)weight[i];
+    } else {
+        float2* const s_stats = reinterpret_cast<float2*>(s_norm);
+        const int lane = threadIdx.x & ((1 << p.log_lanes) - 1), own = min(p.groups, p.G - block * p.groups);
+        for (int q = threadIdx.x >> p.log_lanes; q < own; q += blockDim.x >> p.log_lanes) {
+            const float2 r = norm_join(p, p.parts + ((int64_t)n * p.G + block * p.groups + q) * p.chunks, lane, p.log_lanes);
+            if (lane == 0) s_stats[q] = r;
         }
-        for (; row < end; row += p.lanes_row) store(norm_load<X, FULL>(x + (int64_t)row * p.x_row, valid(row)), row, valid(row));
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < S; ++i) mean[i] = s_stats[group[i]].x;
+#pragma unroll
+        for (int i = 0; i < V; ++i) scale[i] = s_stats[group[ONE ? 0 : i]].y * (float)weight[i];
+    }
+    if (have == 0) return;
+    norm_with(p.act, [&](auto act) HB_INLINE {
+        for (;;) {
+            vec next[U];
+            int have_next = 0;
+            const int here = row;
+            row += U * p.lanes_row;
+            if (row < end) have_next = norm_batch<X, FULL, U>(p, x, row, end, l, next);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u < have) {
+                    const int at = here + u * p.lanes_row;
+                    float y[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) y[i] = act(fmaf((float)v[u][i] - mean[ONE ? 0 : i], scale[i], (float)bias[i]));
+                    norm_store<O, V>(out + (int64_t)at * p.out_row, y, FULL ? V : at == p.rows - 1 ? l.valid_last : l.valid, p.stream);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            if (have_next == 0) break;
+            have = have_next;
+            tk_for<U>([&](auto u) HB_INLINE { v[decltype(u)::value] = next[decltype(u)::value]; });
+        }
     });
 }
 
 // ---------------------------------------------------------------------------
-template <class X, class O, bool FULL, bool ONE>
+template <class X, class O, bool FULL, NormKind KIND>
 static hb_status norm_launch(const NormArgs& a, const NormPlan& plan, hipStream_t st) {
-    constexpr int E = ONE ? 1 : NormVec<X>::V;
+    constexpr int E = kNormEntries<KIND, NormVec<X>::V>;
+    constexpr bool ONE = KIND == kNormOne;
     if (plan.slab) {
         const int64_t wgs = (int64_t)((a.N - 1) / plan.images + 1) * plan.blocks;
         if (!launch_holds((double)wgs, plan.threads)) return HB_ERR_UNSUPPORTED;
         const int lds = (2 * plan.threads * E + 2 * plan.images * plan.groups) * 4;
-        auto kernel = plan.passes <= 1 ? norm_slab_kernel<X, O, 1, FULL, ONE> : plan.passes <= 4 ? norm_slab_kernel<X, O, 4, FULL, ONE> : norm_slab_kernel<X, O, kNormSlots, FULL, ONE>;
+        auto kernel = plan.passes <= 1 ? norm_slab_kernel<X, O, 1, FULL, KIND> : plan.passes <= 4 ? norm_slab_kernel<X, O, 4, FULL, KIND> : norm_slab_kernel<X, O, norm_slots(NormVec<X>::V, ONE), FULL, KIND>;
         if (lds > 65536)
             if (hb_status s = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds)) return s;
         hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(plan.threads), lds, st, a);
         return launch_status();
     }
-    const int64_t wgs = (int64_t)a.N * plan.blocks * plan.chunks;
-    if (!launch_holds((double)wgs, plan.threads) || !launch_holds((double)a.N * a.G, 64)) return HB_ERR_UNSUPPORTED;
+    const int64_t wgs = (int64_t)a.N * plan.blocks * plan.chunks, apply_wgs = (int64_t)a.N * plan.blocks * plan.apply_chunks;
+    if (!launch_holds((double)wgs, plan.threads) || !launch_holds((double)apply_wgs, plan.threads) || !launch_holds((double)a.N * a.G, 64)) return HB_ERR_UNSUPPORTED;
     const int lds = 3 * plan.threads * E * 4;
-    auto stats = norm_stats_kernel<X, FULL, ONE>;
+    auto stats = norm_stats_kernel<X, FULL, KIND>;
     if (lds > 65536)
         if (hb_status s = allow_dynamic_lds(reinterpret_cast<const void*>(stats), lds)) return s;
     hipLaunchKernelGGL(stats, dim3((unsigned)wgs), dim3(plan.threads), lds, st, a);
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(a.N * a.G)), dim3(64), 0, st, a);
-    hipLaunchKernelGGL((norm_apply_kernel<X, O, FULL, ONE>), dim3((unsigned)wgs), dim3(plan.threads), 0, st, a);
+    if (plan.join) {
+        hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(a.N * a.G)), dim3(64), 0, st, a);
+        hipLaunchKernelGGL((norm_apply_kernel<X, O, FULL, ONE, true>), dim3((unsigned)apply_wgs), dim3(plan.threads), 0, st, a);
+    } else {
+        hipLaunchKernelGGL((norm_apply_kernel<X, O, FULL, ONE, false>), dim3((unsigned)apply_wgs), dim3(plan.threads), 8 * plan.groups, st, a);
+    }
     return launch_status();
 }
 
@@ -493,19 +627,31 @@ static hb_status norm_call(NormArgs a, int64_t x_pixel, int64_t out_pixel, void*
     a.passes = plan.passes;
     a.chunk = plan.chunk;
     a.chunks = plan.chunks;
+    a.apply_chunk = plan.apply_chunk;
+    a.apply_chunks = plan.apply_chunks;
+    while (1 << a.log_pixels < plan.pixels) ++a.log_pixels;                 // 1, 2, 4 or 8
     a.x_row = plan.pixels * x_pixel;
     a.out_row = plan.pixels * out_pixel;
     a.lanes_row = plan.threads / (plan.images * plan.width);
     const bool one = a.D % V == 0, full = plan.pixels * (int64_t)a.groups * a.D % V == 0 && (int64_t)a.G * a.D * plan.pixels % V == 0 && a.P % plan.pixels == 0;
-    // as many lanes to a group as there are, up to a wave
-    const int groups = plan.images * plan.groups;
-    while (a.log_lanes < 6 && (groups << a.log_lanes) < plan.threads) ++a.log_lanes;
-    const int size = one ? a.D / V : a.D;
-    a.step_d = (1 << a.log_lanes) % size;
-    a.step_r = (1 << a.log_lanes) / size;
+    a.log_lanes = plan.log_lanes;
+    a.size = one ? a.D / V : a.D >= V ? (a.D - 2) / V + 2 : a.D;
+    a.step_d = (1 << a.log_lanes) % a.size;
+    a.step_r = (1 << a.log_lanes) / a.size;
+    a.by_all = norm_div(plan.images * plan.width);
+    a.by_width = norm_div(plan.width);
+    a.by_size = norm_div(a.size);
+    a.by_D = norm_div(a.D);
+    a.by_blocks = norm_div(plan.blocks);
+    if (!plan.slab) {
+        a.by_chunks = norm_div(plan.chunks);
+        a.by_apply_chunks = norm_div(plan.apply_chunks);
+        a.inverse_P = 1.0 / a.P;
+    }
     a.stream = sizeof(O) <= sizeof(X) && (int64_t)a.groups * a.D * sizeof(O) % 128 == 0 && a.out_row * sizeof(O) % 128 == 0 && a.out_image * sizeof(O) % 128 == 0 && aligned_to(a.out, 128);
-    if (one) return norm_launch<X, O, true, true>(a, plan, st);
-    return full ? norm_launch<X, O, true, false>(a, plan, st) : norm_launch<X, O, false, false>(a, plan, st);
+    if (one) return norm_launch<X, O, true, kNormOne>(a, plan, st);
+    if (a.D >= V) return full ? norm_launch<X, O, true, kNormTwo>(a, plan, st) : norm_launch<X, O, false, kNormTwo>(a, plan, st);
+    return full ? norm_launch<X, O, true, kNormEach>(a, plan, st) : norm_launch<X, O, false, kNormEach>(a, plan, st);
 }
 
 }  // namespace hb

@@ -637,6 +637,8 @@ def hb_group_norm_workspace_size(N, P, C, groups):
 
 def hb_group_norm(x, out, groups, weight=None, bias=None, eps=1e-5, act="none", workspace=None):
     """out = act((x - mean) / sqrt(var + eps) * weight + bias) by groups of channels; x, out: N x P x C or N x H x W x C, fp16 or fp32; out may be x."""
+    if _calls is not None and _calls.group_norm(x, out, groups, weight, bias, eps, act, workspace):
+        return out
     px, tx, (N, P, C), xs = _pixels(x)
     po, to, _, os_ = _pixels(out)
     assert out.shape == x.shape, "output shape"
@@ -654,6 +656,8 @@ def _scales(t, n, what):
 
 def hb_quantize_rows(x, q, scale):
     """Rows of x (M x K fp16) as 8-bit integers q (M x K int8) times scale (M fp32)."""
+    if _calls is not None and _calls.quantize_rows(x, q, scale):
+        return q, scale
     px, M, K, xp = _rows(x, torch.float16)
     pq, Mq, Kq, qp = _rows(q, torch.int8)
     assert (Mq, Kq) == (M, K), "x, q: M x K"
@@ -691,6 +695,8 @@ def _linear_i8(name, x, w, x_scale, w_scale, out, workspace, bias, residual, act
 
 def hb_linear_i8(x, w, x_scale, w_scale, out, workspace=None, bias=None, residual=None, act="none"):
     """out = act(x_scale w_scale (x w^T) + bias) + residual; x: M x K int8, w: N x K int8, a scale per row of each, out and residual: M x N, fp16 or fp32."""
+    if _calls is not None and _calls.linear_i8(x, w, x_scale, w_scale, out, workspace, bias, residual, act):
+        return out
     return _linear_i8("hb_linear_i8", x, w, x_scale, w_scale, out, workspace, bias, residual, act)
 
 
