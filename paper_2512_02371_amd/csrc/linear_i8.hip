@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(256) linear_i8_valu_kernel(LinearArgs<LinI8> p
         for (int j = 0; j < 4; ++j) {
             const int m = m0 + 4 * ty + i, n = n0 + 4 * tx + j;
             if (m >= p.M || n >= p.N) continue;
-            float v = linear_act(lin_scaled(acc[i][j], p.x_scale[m], p.w_scale[n]) + (p.bias ? (float)p.bias[n] : 0.f), p.act);
+            float v = linear_act(lin_scaled(acc[i][j], p.x_scale[m], p.w_scale[n], p.bias ? (float)p.bias[n] : 0.f), p.act);
             if (p.residual) v += (float)static_cast<const O*>(p.residual)[m * p.res_pitch + n];
             static_cast<O*>(p.out)[m * p.out_pitch + n] = (O)v;
         }
@@ -58,7 +58,7 @@ static hb_status linear_i8_prepare(LinearArgs<LinI8>& a, const int8_t* x, const 
 }  // namespace hb
 
 extern "C" size_t hb_linear_i8_workspace_size(int M, int N, int K) {
-    return M < 1 || N < 1 || K < 1 ? 0 : hb::linear_workspace(M, N, hb::LinI8::halves(K));
+    return M < 1 || N < 1 || K < 1 ? 0 : hb::linear_workspace(M, N, hb::LinI8::halves(K), hb::LinI8::costs());
 }
 
 extern "C" hb_status hb_linear_i8_valu(const int8_t* x, const int8_t* w, const float* x_scale, const float* w_scale, const hb_half* bias, const void* residual,

@@ -1,4 +1,4 @@
-// hb_linear: which kernel a call takes and into how many parts the sum over k is split; host arithmetic.
+// hb_linear and hb_linear_i8: which kernel a call takes and into how many parts the sum over k is split; host arithmetic.
 #pragma once
 #include <stddef.h>
 #include <stdint.h>
@@ -44,10 +44,25 @@ constexpr LinCost kLinCostTile64Copied = {64, 64, 0, 0.240, 0.184, 0.27, 0.60, 0
 constexpr double kLinOneStep = 0.72;
 constexpr double kLinLaunch = 2.5, kLinJoin = 2.58, kLinJoinPart = 0.28, kLinJoinRate = 6.9e6;      // us, us, us, bytes per us
 
-inline double linear_cost(LinKernel kernel, int64_t M, int64_t N, int parts, int steps, LinRows rows) {
-    const LinCost& c = kernel == kLinTile128 && rows != kLinCopied  ? kLinCostTile128Held
-                       : kernel == kLinTile64 && rows == kLinCopied ? kLinCostTile64Copied
-                                                                    : kLinCost[kernel];
+// The same for one kind of operands; linear_cost() and linear_plan() take one of these.
+struct LinCosts {
+    LinCost of[kLinKernels], tile64_copied, tile128_held;
+    double one_step, join, join_part, join_rate;
+};
+constexpr LinCosts kLinCostsF16 = {{kLinCost[0], kLinCost[1], kLinCost[2], kLinCost[3], kLinCost[4], kLinCost[5], kLinCost[6]}, kLinCostTile64Copied, kLinCostTile128Held,
+                                   kLinOneStep, kLinJoin, kLinJoinPart, kLinJoinRate};
+// 8-bit integers, a step being 128 k.  Fitted to 5000 calls of the same sizes with every kernel and number of parts, of a half with a residual and a third with fp32 output, as they were launched
+// through ctypes (which no call is faster than; those under 6.3 us were left out).  On 4000 other calls the choice is 3.2 % behind the fastest in the mean, 2.8 % on those of 30 us and more, and 2.2 % with fp16
+// output and no residual; with fp32 output and a residual, which the model leaves out, 6 %.  With the constants above it was 3.6, 5.4, 3.1 and 6 %.
+constexpr LinCosts kLinCostsI8 = {{{16, 16, 16, 0.343, 0.062, 3.03, 0.00, 0.96}, {32, 16, 8, 0.459, 0.148, 2.83, 0.00, 0.81}, {64, 16, 8, 1.076, 0.276, 2.20, 0.00, 0.67},
+                                   {64, 64, 0, 0.346, 0.292, 2.06, 1.21, 0.25}, {128, 64, 0, 0.699, 0.423, 2.29, 1.98, 0.52}, {128, 128, 0, 0.801, 0.538, 1.36, 2.42, 0.00},
+                                   {256, 256, 0, 1.697, 1.664, 9.56, 13.95, 0.00}},
+                                  {64, 64, 0, 0.257, 0.274, 2.16, 0.77, 0.00}, {128, 128, 0, 1.488, 0.998, 2.78, 2.61, 0.00}, 0.95, 1.39, 0.20, 5.6e6};
+
+inline double linear_cost(LinKernel kernel, int64_t M, int64_t N, int parts, int steps, LinRows rows, const LinCosts& costs = kLinCostsF16) {
+    const LinCost& c = kernel == kLinTile128 && rows != kLinCopied  ? costs.tile128_held
+                       : kernel == kLinTile64 && rows == kLinCopied ? costs.tile64_copied
+                                                                    : costs.of[kernel];
     const int64_t wgs = ((M + c.m - 1) / c.m) * ((N + c.n - 1) / c.n) * parts;
     const double slow = rows == kLinOdd ? 1.0 + c.odd : 1.0;
     double t;
@@ -56,13 +71,13 @@ inline double linear_cost(LinKernel kernel, int64_t M, int64_t N, int parts, int
         t = c.begin + (waves > all ? waves : all) * slow;
     } else {
         const double one = steps * c.alone * slow + c.begin, all = (double)((wgs + 255) / 256) * (steps * c.shared * slow + c.end);
-        t = (one > all ? one : all) * (steps == 1 && kernel == kLinTile128x64 ? kLinOneStep : 1.0);
+        t = (one > all ? one : all) * (steps == 1 && kernel == kLinTile128x64 ? costs.one_step : 1.0);
     }
-    if (parts > 1) t += kLinJoin + parts * kLinJoinPart + 8.0 * parts * M * N / kLinJoinRate;
+    if (parts > 1) t += costs.join + parts * costs.join_part + 8.0 * parts * M * N / costs.join_rate;
     return t + kLinLaunch;
 }
 
-inline LinPlan linear_plan(int M, int N, int K, LinRows rows) {
+inline LinPlan linear_plan(int M, int N, int K, LinRows rows, const LinCosts& costs = kLinCostsF16) {
     const int steps = (K - 1) / 64 + 1;
     LinPlan best = {kLinTile64, 1, steps};
     double least = 0.0;
@@ -78,7 +93,7 @@ inline LinPlan linear_plan(int M, int N, int K, LinRows rows) {
         for (int parts : kParts) {
             if (parts > 1 && (kernel == kLinTile256 || wgs * parts > 1024 || steps < (c.waves ? 8 : 2) * parts)) break;
             const int per = (steps - 1) / parts + 1, count = (steps - 1) / per + 1;             // no part is empty
-            const double t = linear_cost(kernel, M, N, count, per, rows);
+            const double t = linear_cost(kernel, M, N, count, per, rows, costs);
             if (!any || t < least) {
                 any = true;
                 least = t;
@@ -90,10 +105,10 @@ inline LinPlan linear_plan(int M, int N, int K, LinRows rows) {
 }
 
 // Bytes for the parts' sums, whatever the rows' addresses.
-inline size_t linear_workspace(int M, int N, int K) {
+inline size_t linear_workspace(int M, int N, int K, const LinCosts& costs = kLinCostsF16) {
     int most = 1;
     for (LinRows rows : {kLinCopied, kLinEven, kLinOdd}) {
-        const int parts = linear_plan(M, N, K, rows).parts;
+        const int parts = linear_plan(M, N, K, rows, costs).parts;
         most = parts > most ? parts : most;
     }
     return most > 1 ? ((size_t)most * M * N * 4 + 255) / 256 * 256 : 0;

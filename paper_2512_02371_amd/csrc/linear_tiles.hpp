@@ -27,6 +27,7 @@ struct LinF16 {
     static __device__ __forceinline__ uint32_t next(uint32_t odd) { return 8 * odd; }        // to the fifth dword where it is wanted
     static __device__ __forceinline__ u32x4 shift(u32x4 v, int d) { return __builtin_bit_cast(u32x4, shift_in_from_right<true>(__builtin_bit_cast(half8, v), d)); }
     static int halves(int K) { return K; }                // the K of hb_linear whose rows have as many bytes
+    static const LinCosts& costs() { return kLinCostsF16; }
 };
 
 // 8-bit integers, sums in 32 bits, a scale for each row of both operands.  A fragment is 16 bytes of a lane as above, twice as many k in the time of one product.
@@ -43,6 +44,7 @@ struct LinI8 {
     static __device__ __forceinline__ uint32_t next(uint32_t odd) { return odd ? 16 : 0; }
     static __device__ __forceinline__ u32x4 shift(u32x4 v, int d) { return shift_in_bytes(v, d); }
     static int halves(int K) { return (K - 1) / 2 + 1; }
+    static const LinCosts& costs() { return kLinCostsI8; }
 };
 
 template <class Op>
@@ -59,9 +61,9 @@ struct LinearArgs {
     const float* w_scale;
 };
 
-// A sum of products of integers, rounded to 24 bits, times its scales.
-__device__ __forceinline__ float lin_scaled(float sum, float xs, float ws) { return sum * xs * ws; }
-__device__ __forceinline__ float lin_scaled(int sum, float xs, float ws) { return (float)sum * xs * ws; }
+// A sum of products, rounded to 24 bits, times its scales, and the bias.
+template <class S>
+__device__ __forceinline__ float lin_scaled(S sum, float xs, float ws, float bias) { return fmaf((float)sum * xs, ws, bias); }
 
 // Four sums of a part.
 __device__ __forceinline__ void lin_store_sums(int* to, intx4 v, int count) {
@@ -105,33 +107,25 @@ __device__ __forceinline__ u32x4 lin_last(const typename Op::T* row, int k, int 
 
 // The epilogue of a wave: its WM x WN sums leave through a patch of LDS that is its own (TILES x 16 rows of WN floats at a time), because a
 // lane holds four columns of one row of a fragment and 16 lanes 16 different rows: from the patch, whole runs of a row are
-// finished and stored, 16 bytes a lane.  The 16-byte pieces of a row stand at piece ^ row % 16 (writes meet no bank twice).
+// finished and stored, 16 bytes a lane.  The 16-byte pieces of a row stand at piece ^ row % 16 (writes meet no bank twice).  Sums of integers meet the scales of
+// their rows of x on the way into the patch, where a lane has one row of a fragment: eight values for 128 rows, requested at once.  What begin() requests, finish() waits for.
 template <class Op, class O, int WM, int WN, int TILES, int BATCH>
-__device__ __forceinline__ void lin_finish(const LinearArgs<Op>& p, O* out, const typename Op::Acc (&acc)[WN / 16][WM / 16], typename Op::Sum* patch, int m0, int n0) {
+struct LinEnd {
     using Acc = typename Op::Acc;
-    constexpr bool kScaled = Op::kScaled && !std::is_same<O, int>::value;      // parts of a sum of integers are stored as they are
+    static constexpr bool kSums = std::is_same<O, int>::value, kScaled = Op::kScaled && !kSums;      // parts of a sum of integers are stored as they are
+    using Patch = typename std::conditional<kSums, Acc, floatx4>::type;
     static_assert(WN >= 32 && (WM / 16) % TILES == 0);
-    constexpr int kFlip = WN / 4 < 16 ? WN / 4 - 1 : 15;
-    constexpr int V = 16 / sizeof(O), kLanes = WN / V, kStep = 64 / kLanes;    // elements and lanes per row, rows per pass
-    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int x = lane % kLanes * V, count = p.N - (n0 + x), r0 = lane / kLanes;
-    float bias[V] = {};
-    if (p.bias) lin_load<V>(bias, p.bias + n0 + x, count);
-    float w_scale[V] = {};
-    if (kScaled) lin_load<V>(w_scale, p.w_scale + n0 + x, count);
-    constexpr int kPasses = 16 * TILES / kStep, kBatch = kPasses < BATCH ? kPasses : BATCH;
-    // the residual and the scales of a batch of rows are requested while the batch before is finished
+    static constexpr int kFlip = WN / 4 < 16 ? WN / 4 - 1 : 15;
+    static constexpr int V = 16 / sizeof(O), kLanes = WN / V, kStep = 64 / kLanes;                   // elements and lanes per row, rows per pass
+    static constexpr int kPasses = 16 * TILES / kStep, kBatch = kPasses < BATCH ? kPasses : BATCH;
     typedef O vec __attribute__((ext_vector_type(V), aligned(sizeof(O))));
-    vec ahead[kBatch] = {}, res[kBatch] = {};
-    float scale_ahead[kBatch] = {}, scale[kBatch] = {};
-    auto request_scales = [&](int first) HB_INLINE {
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int64_t m = m0 + first + b * kStep + r0;
-            if (m < p.M && first < WM) scale_ahead[b] = p.x_scale[m];
-        }
-    };
-    auto request = [&](int first) HB_INLINE {
+    int m0, n0, lane, x, count, r0;
+    float x_scale[kScaled ? WM / 16 : 1], w_scale[V], bias[kScaled ? 1 : V];
+    typedef half_t halves __attribute__((ext_vector_type(V), aligned(2)));
+    halves half_bias;          // beside scales, two to a register
+    vec ahead[kBatch];         // the residual of a batch of rows is requested while the batch before is finished
+
+    __device__ __forceinline__ void request(const LinearArgs<Op>& p, int first) {
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             const int64_t m = m0 + first + b * kStep + r0;
@@ -143,72 +137,115 @@ __device__ __forceinline__ void lin_finish(const LinearArgs<Op>& p, O* out, cons
                     for (int i = 0; i < V; ++i) ahead[b][i] = i < count ? from[i] : (O)0.f;
             }
         }
-    };
-    if (kScaled) request_scales(0);
-    if (p.residual) request(0);
-#pragma unroll 1
-    for (int h = 0; h < WM / 16; h += TILES) {
-        tk_for<WM / 16>([&](auto tile) HB_INLINE {
-            constexpr int j = decltype(tile)::value;
-            if (TILES == WM / 16 || (j / TILES) * TILES == h) {
-                tk_for<WN / 16>([&](auto index) HB_INLINE {
-                    constexpr int i = decltype(index)::value;
-                    *reinterpret_cast<Acc*>(patch + (16 * (j % TILES) + c) * WN + 4 * ((4 * i + g) ^ (c & kFlip))) = acc[i][j];
-                });
-                asm volatile("; fragments %0" ::"n"(j));      // keeps the branches apart: merged, they would index registers
+    }
+    __device__ __forceinline__ void begin(const LinearArgs<Op>& p, int m0_, int n0_) {
+        m0 = m0_;
+        n0 = n0_;
+        lane = threadIdx.x & 63;
+        x = lane % kLanes * V;
+        count = p.N - (n0 + x);
+        r0 = lane / kLanes;
+        if (kScaled) {
+#pragma unroll
+            for (int j = 0; j < WM / 16; ++j) {
+                const int64_t m = (int64_t)m0 + 16 * j + (lane & 15);
+                x_scale[j] = p.x_scale[m < p.M ? m : p.M - 1];
             }
-        });
-        wave_lds_fence();
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w_scale[i] = 0.f;
+            if (!kScaled) bias[i] = 0.f;
+        }
+        half_bias = halves{};
+        if constexpr (kScaled) {
+            lin_load<V>(w_scale, p.w_scale + n0 + x, count);
+            if (p.bias) {
+                if (count >= V) half_bias = *reinterpret_cast<const halves*>(p.bias + n0 + x);
+                else
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (i < count) half_bias[i] = p.bias[n0 + x + i];
+            }
+        } else if (p.bias) {
+            lin_load<V>(bias, p.bias + n0 + x, count);
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) ahead[b] = vec{};
+        if (p.residual) request(p, 0);
+    }
+    __device__ __forceinline__ void finish(const LinearArgs<Op>& p, O* out, const Acc (&acc)[WN / 16][WM / 16], typename Op::Sum* patch) {
+        const int c = lane & 15, g = lane >> 4;
+        vec res[kBatch] = {};
 #pragma unroll 1
-        for (int q = 0; q < kPasses; q += kBatch) {
-            const int first = 16 * h + q * kStep;         // row of the wave
-            if constexpr (std::is_same<O, int>::value) {  // the sums themselves
+        for (int h = 0; h < WM / 16; h += TILES) {
+            tk_for<WM / 16>([&](auto tile) HB_INLINE {
+                constexpr int j = decltype(tile)::value;
+                if (TILES == WM / 16 || (j / TILES) * TILES == h) {
+                    tk_for<WN / 16>([&](auto index) HB_INLINE {
+                        constexpr int i = decltype(index)::value;
+                        Patch v;
+                        if constexpr (kScaled) {
+                            Acc t = acc[i][j];
+                            asm volatile("" : "+v"(t));       // or all of them would be made floats ahead of the loop
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) v[e] = (float)t[e] * x_scale[j];
+                        } else {
+                            v = acc[i][j];
+                        }
+                        *reinterpret_cast<Patch*>(patch + (16 * (j % TILES) + c) * WN + 4 * ((4 * i + g) ^ (c & kFlip))) = v;
+                    });
+                    asm volatile("; fragments %0" ::"n"(j));  // keeps the branches apart: merged, they would index registers
+                }
+            });
+            wave_lds_fence();
+#pragma unroll 1
+            for (int q = 0; q < kPasses; q += kBatch) {
+                const int first = 16 * h + q * kStep;     // row of the wave
+                if constexpr (kSums) {
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b) {
+                        const int r = (q + b) * kStep + r0;
+                        const Acc t = *reinterpret_cast<const Acc*>(patch + r * WN + 4 * ((x / 4) ^ (r & kFlip)));
+                        const int64_t m = m0 + first + b * kStep + r0;
+                        if (m < p.M && count > 0) lin_store_sums(out + m * p.out_pitch + n0 + x, t, count);
+                    }
+                    continue;
+                }
+                float v[kBatch][V];
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b) {
                     const int r = (q + b) * kStep + r0;
-                    const Acc t = *reinterpret_cast<const Acc*>(patch + r * WN + 4 * ((x / 4) ^ (r & kFlip)));
+#pragma unroll
+                    for (int e = 0; e < V; e += 4) {
+                        const Patch t = *reinterpret_cast<const Patch*>(patch + r * WN + 4 * (((x + e) / 4) ^ (r & kFlip)));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[b][e + i] = kScaled ? fmaf(t[i], w_scale[e + i], (float)half_bias[e + i]) : t[i] + bias[kScaled ? 0 : e + i];     // as lin_scaled
+                    }
+                }
+                if (!kScaled && p.residual) {
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b) res[b] = ahead[b];
+                    request(p, first + kBatch * kStep);
+                }
+                lin_act<kBatch * V>(reinterpret_cast<float(&)[kBatch * V]>(v), p.act);
+                if (p.residual) {
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) v[b][i] += (float)(kScaled ? ahead : res)[b][i];
+                    if (kScaled) request(p, first + kBatch * kStep);         // after it: the scales leave no registers for a copy
+                }
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) {
                     const int64_t m = m0 + first + b * kStep + r0;
-                    if (m < p.M && count > 0) lin_store_sums(out + m * p.out_pitch + n0 + x, t, count);
-                }
-                continue;
-            }
-            float v[kBatch][V];
-            if (kScaled) {
-#pragma unroll
-                for (int b = 0; b < kBatch; ++b) scale[b] = scale_ahead[b];
-                request_scales(first + kBatch * kStep);
-            }
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                const int r = (q + b) * kStep + r0;
-#pragma unroll
-                for (int e = 0; e < V; e += 4) {
-                    const Acc t = *reinterpret_cast<const Acc*>(patch + r * WN + 4 * (((x + e) / 4) ^ (r & kFlip)));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[b][e + i] = (kScaled ? lin_scaled(t[i], scale[b], w_scale[e + i]) : (float)t[i]) + bias[e + i];
+                    if (m < p.M && count > 0) lin_store<V>(out + m * p.out_pitch + n0 + x, v[b], count);
                 }
             }
-            if (p.residual) {
-#pragma unroll
-                for (int b = 0; b < kBatch; ++b) res[b] = ahead[b];
-                request(first + kBatch * kStep);
-            }
-            lin_act<kBatch * V>(reinterpret_cast<float(&)[kBatch * V]>(v), p.act);
-            if (p.residual) {
-#pragma unroll
-                for (int b = 0; b < kBatch; ++b)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) v[b][i] += (float)res[b][i];
-            }
-#pragma unroll
-            for (int b = 0; b < kBatch; ++b) {
-                const int64_t m = m0 + first + b * kStep + r0;
-                if (m < p.M && count > 0) lin_store<V>(out + m * p.out_pitch + n0 + x, v[b], count);
-            }
+            wave_lds_fence();
         }
-        wave_lds_fence();
     }
-}
+};
 constexpr int kLinPatch = 1;                              // fragments of 16 rows in a patch
 
 // Which tile a workgroup takes: groups of 8 tile rows, column after column, in the order in which the workgroups of one XCD follow
@@ -324,6 +361,10 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
 
     const int wm = wv / (BN / WN) * WM, wn = wv % (BN / WN) * WN;
     const uint32_t at_x = (uint32_t)(wm + c) * 128 + 16 * (g ^ lin_flip(c)), at_w = (uint32_t)(BM + wn + c) * 128 + 16 * (g ^ lin_flip(c));
+    // scales and the first of the residual are requested ahead of the rows (32768 x 1024, K 1024 with a residual 66 -> 62 us), where there are registers for them
+    LinEnd<Op, O, WM, WN, kLinPatch, 4> end;
+    constexpr bool kEarly = Op::kScaled && sizeof(O) == 2;
+    if (kEarly) end.begin(p, m0 + wm, n0 + wn);
     auto compute = [&](int buf) HB_INLINE {
         const char* base = s_tiles + buf * kStage;
 #pragma unroll
@@ -401,8 +442,8 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
         compute(s & 1);
     }
     lds_barrier();
-    lin_finish<Op, O, WM, WN, kLinPatch, 4>(p, static_cast<O*>(p.out) + (int64_t)blockIdx.y * p.M * p.out_pitch, acc,
-                                            reinterpret_cast<typename Op::Sum*>(s_tiles) + 16 * kLinPatch * WN * wv, m0 + wm, n0 + wn);
+    if (!kEarly) end.begin(p, m0 + wm, n0 + wn);
+    end.finish(p, static_cast<O*>(p.out) + (int64_t)blockIdx.y * p.M * p.out_pitch, acc, reinterpret_cast<typename Op::Sum*>(s_tiles) + 16 * kLinPatch * WN * wv);
 }
 
 // The large tile: 256 x 256 outputs, four waves of 128 x 128, one to a SIMD.  A wave reads 16 fragments from LDS for 64 products (half of
@@ -531,7 +572,9 @@ __global__ void __launch_bounds__(256, 1) linear_large_kernel(LinearArgs<Op> p) 
         }
         int tm, tn;
         lin_tile(tile, tiles_m, tiles_n, tm, tn);
-        lin_finish<Op, O, 128, 128, kLinPatch, Op::kScaled ? 2 : 4>(p, static_cast<O*>(p.out), acc, reinterpret_cast<typename Op::Sum*>(s_tiles + 2 * kStage) + 2048 * wv, tm * BM + wm, tn * BN + wn);
+        LinEnd<Op, O, 128, 128, kLinPatch, 4> end;
+        end.begin(p, tm * BM + wm, tn * BN + wn);
+        end.finish(p, static_cast<O*>(p.out), acc, reinterpret_cast<typename Op::Sum*>(s_tiles + 2 * kStage) + 2048 * wv);
     }
     tk_wait_loads<0>();                                   // nothing may arrive in LDS that is no longer this workgroup's
 }
@@ -556,19 +599,16 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs<Op> p, cons
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] += part[i];
     }
+    float bias[V] = {};
+    if (p.bias) lin_load<V>(bias, p.bias + n, have);
     if (Op::kScaled) {
         const float scale = p.x_scale[m];
         lin_load<V>(q, p.w_scale + n, have);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = lin_scaled(sum[i], scale, q[i]);
+        for (int i = 0; i < V; ++i) v[i] = lin_scaled(sum[i], scale, q[i], bias[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = sum[i];
-    }
-    if (p.bias) {
-        lin_load<V>(q, p.bias + n, have);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += q[i];
+        for (int i = 0; i < V; ++i) v[i] = sum[i] + bias[i];
     }
     lin_act<V>(v, p.act);
     if (p.residual) {
@@ -635,8 +675,8 @@ __global__ void __launch_bounds__(64 * WAVES) linear_rows_kernel(LinearArgs<Op> 
             static_cast<int*>(p.out)[((int64_t)blockIdx.y * p.M + r) * p.out_pitch + n] = sum;
             continue;
         }
-        float v = Op::kScaled ? lin_scaled(sum, p.x_scale[r], p.w_scale[n]) : (float)sum;
-        if (p.bias) v += (float)p.bias[n];
+        const float bias = p.bias ? (float)p.bias[n] : 0.f;
+        float v = Op::kScaled ? lin_scaled(sum, p.x_scale[r], p.w_scale[n], bias) : (float)sum + bias;
         v = linear_act(v, p.act);
         if (p.residual) v += (float)static_cast<const O*>(p.residual)[r * p.res_pitch + n];
         static_cast<O*>(p.out)[((int64_t)blockIdx.y * p.M + r) * p.out_pitch + n] = (O)v;
@@ -689,7 +729,7 @@ static hb_status linear_run(const LinPlan& plan, LinRows rows, const LinearArgs<
                    : odd              ? linear_launch<Op, O, 64, 64, 16, 32, kLinOdd, 1>(a, parts, st)
                                       : linear_launch<Op, O, 64, 64, 16, 32, kLinEven, 1>(a, parts, st);
         case kLinTile128x64: return odd ? linear_launch<Op, O, 128, 64, 32, 64, kLinOdd, 1>(a, parts, st) : linear_launch<Op, O, 128, 64, 32, 64, kLinEven, 1>(a, parts, st);
-        case kLinTile128: return rows == kLinCopied ? linear_launch<Op, O, 128, 128, 64, 32, kLinCopied, 1>(a, parts, st) : linear_launch<Op, O, 128, 128, 64, 32, kLinOdd, 1>(a, parts, st);
+        case kLinTile128: return rows == kLinCopied ? linear_launch<Op, O, 128, 128, sizeof(O) == 2 && Op::kScaled ? 32 : 64, sizeof(O) == 2 && Op::kScaled ? 64 : 32, kLinCopied, 1>(a, parts, st) : linear_launch<Op, O, 128, 128, 64, 32, kLinOdd, 1>(a, parts, st);
         default: return linear_launch_large<Op, O>(a, st);
     }
 }
@@ -699,9 +739,9 @@ static hb_status linear_call(const LinearArgs<Op>& a, void* workspace, size_t wo
     const LinRows rows = aligned_to(a.x, 16) && aligned_to(a.w, 16) && (pitches | a.K) % Op::kPer == 0 ? kLinCopied
                          : aligned_to(a.x, 4) && aligned_to(a.w, 4) && pitches % (Op::kPer / 4) == 0        ? kLinEven
                                                                                                 : kLinOdd;
-    if (const size_t need = linear_workspace(a.M, a.N, Op::halves(a.K)))
+    if (const size_t need = linear_workspace(a.M, a.N, Op::halves(a.K), Op::costs()))
         if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need) return HB_ERR_WORKSPACE;
-    const LinPlan plan = linear_plan(a.M, a.N, Op::halves(a.K), rows);
+    const LinPlan plan = linear_plan(a.M, a.N, Op::halves(a.K), rows, Op::costs());
     LinearArgs<Op> b = a;
     b.steps = plan.steps;
     if (plan.parts == 1) return linear_run<Op, O>(plan, rows, b, 1, st);
