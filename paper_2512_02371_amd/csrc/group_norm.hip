@@ -70,15 +70,31 @@ __device__ __forceinline__ NormLane norm_lane(const NormArgs& p, int first_image
     return l;
 }
 
-// V adjacent elements, zeros from `valid` on; `from` is not read where that is 0.
+// N elements, put at AT of a vector.
+template <int AT, int N, class vec, class T>
+__device__ __forceinline__ void norm_piece(vec& r, const T* from) {
+    typedef T piece __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    const piece q = *reinterpret_cast<const piece*>(from);
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[AT + i] = q[i];
+}
+// V adjacent elements, zeros from `valid` on; `from` is not read where that is 0.  What is less than a vector comes in pieces of four, two and one.
 template <class X, bool FULL>
 __device__ __forceinline__ typename NormVec<X>::type norm_load(const X* from, int valid) {
     using vec = typename NormVec<X>::type;
-    if (FULL || valid == NormVec<X>::V) return *reinterpret_cast<const vec*>(from);
+    constexpr int V = NormVec<X>::V;
+    if (FULL || valid == V) return *reinterpret_cast<const vec*>(from);
     vec r = {};
-#pragma unroll
-    for (int i = 0; i < NormVec<X>::V; ++i)
-        if (i < valid) r[i] = from[i];
+    if (V == 8 && valid & 4) {
+        norm_piece<0, 4>(r, from);
+        if (valid & 2) norm_piece<V == 8 ? 4 : 0, 2>(r, from + 4);
+        if (valid == 7) norm_piece<V == 8 ? 6 : 0, 1>(r, from + 6);
+        if (valid == 5) norm_piece<V == 8 ? 4 : 0, 1>(r, from + 4);
+    } else {
+        if (valid & 2) norm_piece<0, 2>(r, from);
+        if (valid == 3) norm_piece<2, 1>(r, from + 2);
+        if (valid == 1) norm_piece<0, 1>(r, from);
+    }
     return r;
 }
 
@@ -133,9 +149,25 @@ __device__ __forceinline__ void norm_fold(const float (&v)[KIND == kNormOne ? 1 
         for (int i = 0; i < kNormEntries<KIND, V>; ++i) to[i] = v[i];
     }
 }
-// Sum over the lanes that share a group, the same in all of them.
+// Sum over the 2^log_lanes lanes that share a group, the same in all of them.  Within 16 lanes by their neighbours' registers, then between quarters and halves of the
+// wave; through LDS each step would wait for it.
+template <int CTRL>
+__device__ __forceinline__ float norm_dpp(float v) {
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float norm_lanes_sum(float v, int log_lanes) {
-    for (int m = 1 << log_lanes >> 1; m > 0; m >>= 1) v += __shfl_xor(v, m);
+    if (log_lanes > 0) v = norm_dpp<0xb1>(v);             // quad_perm 1 0 3 2
+    if (log_lanes > 1) v = norm_dpp<0x4e>(v);             // quad_perm 2 3 0 1
+    if (log_lanes > 2) v = norm_dpp<0x141>(v);            // row_half_mirror: the other four of eight
+    if (log_lanes > 3) v = norm_dpp<0x140>(v);            // row_mirror: the other eight of 16
+    if (log_lanes > 4) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
+        v = __builtin_bit_cast(float, (int)s[0]) + __builtin_bit_cast(float, (int)s[1]);
+    }
+    if (log_lanes > 5) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, v), __builtin_bit_cast(int, v), false, false);
+        v = __builtin_bit_cast(float, (int)s[0]) + __builtin_bit_cast(float, (int)s[1]);
+    }
     return v;
 }
 
@@ -187,10 +219,26 @@ __device__ __forceinline__ void norm_store(O* to, const float (&v)[V], int valid
         for (int i = 0; i < V; ++i) q[i] = (O)v[i];
         if (stream) __builtin_nontemporal_store(q, reinterpret_cast<vec*>(to));
         else *reinterpret_cast<vec*>(to) = q;
-    } else {
+    } else {                                              // in pieces of four, two and one
+        auto piece = [&](auto at, auto n) HB_INLINE {
+            constexpr int AT = decltype(at)::value, N = decltype(n)::value;
+            typedef O part __attribute__((ext_vector_type(N), aligned(sizeof(O))));
+            part q;
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < valid) to[i] = (O)v[i];
+            for (int i = 0; i < N; ++i) q[i] = (O)v[AT + i];
+            *reinterpret_cast<part*>(to + AT) = q;
+        };
+        constexpr int H = V == 8 ? 4 : 0;
+        if (V == 8 && valid & 4) {
+            piece(TkInt<0>{}, TkInt<4>{});
+            if (valid & 2) piece(TkInt<H>{}, TkInt<2>{});
+            if (valid == 7) piece(TkInt<H + 2>{}, TkInt<1>{});
+            if (valid == 5) piece(TkInt<H>{}, TkInt<1>{});
+        } else {
+            if (valid & 2) piece(TkInt<0>{}, TkInt<2>{});
+            if (valid == 3) piece(TkInt<2>{}, TkInt<1>{});
+            if (valid == 1) piece(TkInt<0>{}, TkInt<1>{});
+        }
     }
 }
 // f(activation) with the call's activation: one branch for all that f does.
@@ -350,10 +398,10 @@ __device__ __forceinline__ int norm_batch(const NormArgs& p, const X* x, int row
     return have;
 }
 
-template <class X, bool FULL, NormKind KIND>
-__global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs p) {
+template <class X, bool FULL, NormKind KIND, int MOST>
+__global__ void __launch_bounds__(MOST) norm_stats_kernel(NormArgs p) {
     using vec = typename NormVec<X>::type;
-    constexpr int V = NormVec<X>::V, E = kNormEntries<KIND, V>, U = FULL ? kNormBatch : kNormBatch / 2;
+    constexpr int V = NormVec<X>::V, E = kNormEntries<KIND, V>, U = FULL && MOST < kNormThreads ? kNormBatch : kNormBatch / 2;
     constexpr bool ONE = KIND == kNormOne;
     extern __shared__ float s_norm[];
     const int nT = blockDim.x;
@@ -425,16 +473,15 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs p) {
         float c = 0.f, m = 0.f, left = 0.f, s = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float k = in(i) ? count + extra[i] : 0.f;
-            c += k;
-            m = fmaf(k, mean[i], m);
+            c += in(i) ? count + extra[i] : 0.f;
+            m += in(i) ? (count + extra[i]) * mean[i] : 0.f;                 // what is behind the row may be anything
         }
         const float inverse = c > 0.f ? 1.f / c : 0.f;
         m *= inverse;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float k = in(i) ? count + extra[i] : 0.f, d = mean[i] - m;
-            left = fmaf(k, d, left);
+            const float k = count + extra[i], d = mean[i] - m;
+            left += in(i) ? k * d : 0.f;
             s += in(i) ? fmaf(k * d, d, squares[i]) : 0.f;
         }
         left *= inverse;
@@ -457,22 +504,18 @@ __global__ void __launch_bounds__(kNormThreads) norm_stats_kernel(NormArgs p) {
     }
     __syncthreads();
     const int lane = threadIdx.x & ((1 << p.log_lanes) - 1);
+    const float c = (float)(min((begin + p.chunk) << p.log_pixels, p.P) - (begin << p.log_pixels)) * (float)p.D, inverse_c = 1.f / c;     // elements of a group in the chunk
     for (int q = threadIdx.x >> p.log_lanes; q < p.groups; q += nT >> p.log_lanes) {
-        float c = 0.f, m = 0.f;
-        norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE {
-            const float k = there ? s_count[e] : 0.f;
-            c += k;
-            m = fmaf(k, s_mean[e], m);
-        });
-        c = norm_lanes_sum(c, p.log_lanes);
-        m = norm_lanes_sum(m, p.log_lanes) / c;
+        float m = 0.f;
+        norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE { m += there ? s_count[e] * s_mean[e] : 0.f; });
+        m = norm_lanes_sum(m, p.log_lanes) * inverse_c;
         float left = 0.f, s = 0.f;
         norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE {
-            const float d = s_mean[e] - m, cd = there ? s_count[e] * d : 0.f;
-            left += cd;
+            const float d = s_mean[e] - m, cd = s_count[e] * d;
+            left += there ? cd : 0.f;
             s += there ? fmaf(cd, d, s_squares[e]) : 0.f;
         });
-        left = norm_lanes_sum(left, p.log_lanes) / c;
+        left = norm_lanes_sum(left, p.log_lanes) * inverse_c;
         s = norm_lanes_sum(s, p.log_lanes);
         const int g = block * p.groups + q;
         if (lane == 0 && g < p.G) p.parts[((int64_t)n * p.G + g) * p.chunks + chunk] = float2{m + left, fmaf(-c * left, left, s)};
@@ -596,7 +639,7 @@ static hb_status norm_launch(const NormArgs& a, const NormPlan& plan, hipStream_
     const int64_t wgs = (int64_t)a.N * plan.blocks * plan.chunks, apply_wgs = (int64_t)a.N * plan.blocks * plan.apply_chunks;
     if (!launch_holds((double)wgs, plan.threads) || !launch_holds((double)apply_wgs, plan.threads) || !launch_holds((double)a.N * a.G, 64)) return HB_ERR_UNSUPPORTED;
     const int lds = 3 * plan.threads * E * 4;
-    auto stats = norm_stats_kernel<X, FULL, KIND>;
+    auto stats = plan.threads <= 256 ? norm_stats_kernel<X, FULL, KIND, 256> : norm_stats_kernel<X, FULL, KIND, kNormThreads>;
     if (lds > 65536)
         if (hb_status s = allow_dynamic_lds(reinterpret_cast<const void*>(stats), lds)) return s;
     hipLaunchKernelGGL(stats, dim3((unsigned)wgs), dim3(plan.threads), lds, st, a);
