@@ -84,7 +84,8 @@ __device__ __forceinline__ typename NormVec<X>::type norm_load(const X* from, in
     using vec = typename NormVec<X>::type;
     constexpr int V = NormVec<X>::V;
     if (FULL || valid == V) return *reinterpret_cast<const vec*>(from);
-    vec r = {};
+    typedef X whole __attribute__((ext_vector_type(V)));
+    whole r = {};
     if (V == 8 && valid & 4) {
         norm_piece<0, 4>(r, from);
         if (valid & 2) norm_piece<V == 8 ? 4 : 0, 2>(r, from + 4);
