@@ -323,46 +323,37 @@ __global__ void __launch_bounds__(kNormThreads) norm_slab_kernel(NormArgs p) {
         if (lane == 0) s_mean[q] = sum / first;
     }
     lds_barrier();
-    // Twice only where the first vectors say so little of the others that the squares about them have lost digits: more than four deviations from the mean.
+    // The first vectors are at least a 16th of all: where their mean is off by e, that is a difference between them and the others that is in the variance too, 15 var >= e^2, and
+    // the squares about it are at most 16 times those about the mean.
     float mean[S];
-    for (int again = 0;; ++again) {
 #pragma unroll
-        for (int i = 0; i < SLOTS; ++i) asm volatile("" : "+v"(held[i]));    // or their conversions would be kept from turn to turn, in registers that there are not
+    for (int i = 0; i < S; ++i) mean[i] = s_mean[group[i]], a[i] = 0.f;
+    rows([&](const vec& v, int, int valid) HB_INLINE {
 #pragma unroll
-        for (int i = 0; i < S; ++i) mean[i] = s_mean[group[i]], a[i] = b[i] = 0.f;
-        rows([&](const vec& v, int, int valid) HB_INLINE {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = FULL || i < valid ? (float)v[i] - mean[ONE ? 0 : i] : 0.f;
-                a[ONE ? 0 : i] += d;
-                b[ONE ? 0 : i] = fmaf(d, d, b[ONE ? 0 : i]);
-            }
+        for (int i = 0; i < V; ++i) {
+            const float d = FULL || i < valid ? (float)v[i] - mean[ONE ? 0 : i] : 0.f;
+            a[ONE ? 0 : i] += d;
+            b[ONE ? 0 : i] = fmaf(d, d, b[ONE ? 0 : i]);
+        }
+    });
+    norm_fold<V, KIND>(a, cut, s_a + threadIdx.x * E);
+    norm_fold<V, KIND>(b, cut, s_b + threadIdx.x * E);
+    __syncthreads();
+    for (int q = threadIdx.x >> p.log_lanes; q < nG; q += nT >> p.log_lanes) {
+        float left = 0.f, squares = 0.f;
+        norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE {
+            left += there ? s_a[e] : 0.f;
+            squares += there ? s_b[e] : 0.f;
         });
-        norm_fold<V, KIND>(a, cut, s_a + threadIdx.x * E);
-        norm_fold<V, KIND>(b, cut, s_b + threadIdx.x * E);
-        __syncthreads();
-        int far = 0;
-        for (int q = threadIdx.x >> p.log_lanes; q < nG; q += nT >> p.log_lanes) {
-            float left = 0.f, squares = 0.f;
-            norm_entries<V, KIND>(p, q, lane, [&](int e, bool there) HB_INLINE {
-                left += there ? s_a[e] : 0.f;
-                squares += there ? s_b[e] : 0.f;
-            });
-            left = norm_lanes_sum(left, p.log_lanes) / count;
-            squares = norm_lanes_sum(squares, p.log_lanes) / count;
-            const float var = fmaxf(squares - left * left, 0.f);
-            far |= left * left > 16.f * var;
-            if (lane == 0) {
-                s_mean[q] += left;
-                s_rstd[q] = 1.f / sqrtf(var + p.eps);
-            }
+        left = norm_lanes_sum(left, p.log_lanes) / count;
+        squares = norm_lanes_sum(squares, p.log_lanes) / count;
+        if (lane == 0) {
+            s_mean[q] += left;
+            const float var = squares - left * left;      // a NaN, as an infinity makes of it, stays one
+            s_rstd[q] = 1.f / sqrtf((var < 0.f ? 0.f : var) + p.eps);
         }
-        if (p.passes == 1 || again == 1) {
-            __syncthreads();
-            break;
-        }
-        if (!__syncthreads_or(far)) break;
     }
+    __syncthreads();
     float scale[V];
 #pragma unroll
     for (int i = 0; i < S; ++i) mean[i] = s_mean[group[i]];

@@ -7,7 +7,7 @@ namespace hb {
 
 constexpr int kNormThreads = 1024;        // most of a workgroup
 // Most vectors of a lane that stay in registers, 256 KB of a workgroup of 1024; fewer where each element of a vector of 8 has sums of its own.
-constexpr int norm_slots(int V, bool one) { return V == 8 && !one ? 10 : 16; }
+constexpr int norm_slots(int V, bool one) { return V == 8 && !one ? 14 : 16; }
 constexpr int kNormWorkgroups = 512;      // that read chunks of streaming rows
 constexpr int kNormJoin = 8;              // chunks of a lane that joins them
 constexpr int kNormFewChunks = 64;        // of a group, that need no launch to be joined

@@ -42,7 +42,7 @@ def test_group_norm(plans):
         assert p["log_lanes"] <= 6 and (p["threads"] >> p["log_lanes"]) >= 1 and (groups << p["log_lanes"]) < 2 * p["threads"] or p["log_lanes"] == 0, what
         E = 1 if D % V == 0 else 2 if D >= V else V
         if p["slab"]:
-            assert (p["passes"] - 1) * across < p["rows"] <= p["passes"] * across and p["passes"] <= (10 if V == 8 and E > 1 else 16), what
+            assert (p["passes"] - 1) * across < p["rows"] <= p["passes"] * across and p["passes"] <= (14 if V == 8 and E > 1 else 16), what
             assert p["images"] == 1 or p["groups"] == G, what
             assert 4 * (2 * p["threads"] * E + 2 * groups) <= 160 * 1024, what
         else:
