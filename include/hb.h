@@ -385,7 +385,7 @@ hb_status hb_pyr_level_valu(const hb_half *in, float *residual, hb_half *down_or
                             hb_stream stream);
 
 /*
- * Token operators.  What turns the pixels of a feature map (hb_conv3x3) into tokens and lets them look at the states of an
+ * Token operators (and, further down, the operators around a feature map).  What turns the pixels of a feature map (hb_conv3x3) into tokens and lets them look at the states of an
  * encoder: a matrix product with its epilogue, rotary positions on several axes, attention to states of another length.
  * Forward passes, like every stage here.  The conventions above hold (device pointers, one stream, no allocation, no
  * synchronisation, validated before any HIP call); all sums, softmax statistics and angles are fp32.
@@ -472,7 +472,7 @@ hb_status hb_attention_valu(const hb_half *q, const hb_half *k, const hb_half *v
  * N, P, C >= 1; D at most HB_GROUP_NORM_MAX_CHANNELS, P and N * groups less than 2^30 (HB_ERR_UNSUPPORTED beyond; offsets may pass 2^32).  Base pointers need the
  * alignment of their elements; fastest with 16-byte aligned pixels.
  * `workspace`: device scratch of at least hb_group_norm_workspace_size(N, P, C, groups) bytes, 256-byte aligned, contents undefined on exit; concurrent
- * calls need their own.  The size is 0, and the pointer may be NULL, where the pixels of a group fit a compute unit.
+ * calls need their own.  The size is 0, and the pointer may be NULL, where a group's pixels are few (whatever the types and strides).
  */
 size_t hb_group_norm_workspace_size(int N, int P, int C, int groups);
 hb_status hb_group_norm(const void *x, hb_type x_type, const hb_half *weight_or_null, const hb_half *bias_or_null, void *out, hb_type out_type,
