@@ -52,7 +52,7 @@ inline NormPlan norm_plan(int N, int P, int C, int G, int V, bool dense) {
     p.groups = least;
     // A slab's time is that of its workgroup, whose one compute unit has some 0.07 us of arithmetic and transfers for a KB (0.13 where the elements of a vector have sums of their
     // own), or that of all the bytes, 0.42 us a MB, and 5 us besides; reading twice takes 10 us and 0.52 a MB.  Fitted to 30 calls, silu, of 1 x 64 x 512 to 8 x 4096 x 1024
-    // in 32 groups; 2 x 1024 x 640 15.0 us as slabs of 80 KB and 11.4 read twice, 16 x 256 x 1280 10.8 of 20 KB and 15.0, 1 x 16384 x 256 48 and 12.8.
+    // in 32 groups; 2 x 1024 x 640 14.3 us as slabs of 80 KB and 10.6 read twice, 16 x 256 x 1280 9.9 of 20 KB and 14.5, 1 x 16384 x 256 48 and 12.8.
     const double all_MB = (double)N * P * C * size / 1e6;
     const auto slab = [&](int groups) {
         const double kb = (double)width(groups) * p.rows * 0.016, alone = 5.0 + kb * (D % V == 0 ? 0.065 : 0.125), all = 5.5 + 0.42 * all_MB;
@@ -103,7 +103,7 @@ inline NormPlan norm_plan(int N, int P, int C, int G, int V, bool dense) {
         chunks = (p.rows - 1) / chunk + 1;
     };
     // a workgroup to a compute unit, so that few parts are joined, where that is a large part of the time (1 x 16384 x 256 12.8 us, with twice as many 14.1, with twice and eight times as
-    // many 14.8; 8 x 4096 x 320 21.8, 22.1, 25.7); else enough for some to read while others write (2^20 x 64 with 512 and 2048 85.7, with 256 and 1024 89)
+    // many 14.8; 8 x 4096 x 320 21.8, 22.1, 25.7); else enough for some to read while others write (2^20 x 64 with 512 and 2048 4 % faster than with 256 and 1024)
     const bool many = all_MB >= 64;
     share(2, many ? kNormWorkgroups : kNormWorkgroups / 2, p.chunk, p.chunks);
     share(2, many ? 4 * kNormWorkgroups : kNormWorkgroups / 2, p.apply_chunk, p.apply_chunks);
