@@ -468,7 +468,8 @@ hb_status hb_attention_valu(const hb_half *q, const hb_half *k, const hb_half *v
  * in any order; that of a single image or pixel has no meaning).  out may be x itself, of one type and with its strides (in place).
  * weight, bias: C fp16 values, or NULL for ones and zeros.  eps > 0.  groups 1 is a norm over whole images, and with P = 1 over the channels of each token.
  * Statistics are fp32, the variance of the differences from the mean (a mean far from zero costs no digits of it but those of the mean itself); one
- * rounding at the end.  A NaN or an infinity makes NaN of its image's group alone.  fp32 values must be such that the sum of the squares of a group's differences holds in fp32.
+ * rounding at the end.  A NaN or an infinity makes NaN of its image's group alone.  Of fp32 values the sum of a group's magnitudes, and 16 times the
+ * sum of the squares of its differences from the mean, must hold in fp32.
  * N, P, C >= 1; D at most HB_GROUP_NORM_MAX_CHANNELS, P and N * groups less than 2^30 (HB_ERR_UNSUPPORTED beyond; offsets may pass 2^32).  Base pointers need the
  * alignment of their elements; fastest with 16-byte aligned pixels.
  * `workspace`: device scratch of at least hb_group_norm_workspace_size(N, P, C, groups) bytes, 256-byte aligned, contents undefined on exit; concurrent

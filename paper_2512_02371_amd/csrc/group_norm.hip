@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(MOST) norm_stats_kernel(NormArgs p) {
                         }
                         const float d = m - mean[i];
                         mean[i] = fmaf(d, f, mean[i]);
-                        squares[i] += fmaf(d * d, g, s);
+                        squares[i] += fmaf(d * g, d, s);                     // g is 0 ahead of a lane's first batch, and d the whole mean: its square may pass fp32
                     }
                 };
                 if (have == U) join(TkInt<1>{});
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(MOST) norm_stats_kernel(NormArgs p) {
                 if (i < l.valid_last) {
                     const float d = (float)v[i] - mean[i];
                     mean[i] = fmaf(d, f, mean[i]);
-                    squares[i] = fmaf(d * d, count * f, squares[i]);
+                    squares[i] = fmaf(d * (count * f), d, squares[i]);       // as above
                     extra[i] = 1.f;
                 }
         }
