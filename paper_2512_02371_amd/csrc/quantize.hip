@@ -1,6 +1,7 @@
 // hb_quantize_rows: rows of fp16 values as 8-bit integers with a scale.
 #include "hb_device.hpp"
 #include "hb_host.hpp"
+#include "quantize_plan.hpp"
 
 namespace hb {
 
@@ -19,8 +20,6 @@ __device__ __forceinline__ float quantized(float x, float top, float inverse) {
     const float t = 127.f * x, q = t * inverse;
     return rintf(fmaf(fmaf(-q, top, t), inverse, q));
 }
-
-constexpr int kQuantizeHeld = 8;          // vectors of a lane that stay in registers
 
 // Eight adjacent values at any address, zeros from `valid` on (in pieces of four, two and one), and their integers.  WHOLE: all eight are there.
 template <bool WHOLE>
@@ -121,20 +120,20 @@ constexpr int kQuantizeMostK = 0x7fffffff - (1 << 17) + 1;                     /
 
 template <int LANES>
 static hb_status quantize_launch(const QuantizeArgs& a, hipStream_t st) {
-    constexpr int kRows = LANES > 256 ? 1 : 256 / LANES;
-    const dim3 grid((unsigned)((a.M - 1) / kRows + 1)), block(LANES > 256 ? LANES : 256);
+    const dim3 grid((unsigned)quantize_workgroups(a.M, LANES)), block(quantize_threads(LANES));
     if (a.K % 8 == 0) hipLaunchKernelGGL((quantize_rows_kernel<LANES, true>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((quantize_rows_kernel<LANES, false>), grid, block, 0, st, a);
     return launch_status();
 }
-
-// So many lanes that each has two vectors of a row, up to a wave; more waves where a wave does not hold the row, and where rows are so few that one is read sooner by several
-// (91824 x 35 with a wave each 33 us).
 static hb_status quantize_call(const QuantizeArgs& a, hipStream_t st) {
-    const int M = a.M, K = a.K;
-    if (K > 8 * 256 * kQuantizeHeld || (M < 64 && K > 4096)) return quantize_launch<1024>(a, st);
-    if (K > 8 * 64 * kQuantizeHeld || (M < 1024 && K > 512)) return quantize_launch<256>(a, st);
-    return K <= 128 ? quantize_launch<8>(a, st) : K <= 256 ? quantize_launch<16>(a, st) : K <= 512 ? quantize_launch<32>(a, st) : quantize_launch<64>(a, st);
+    switch (quantize_lanes(a.M, a.K)) {
+        case 8: return quantize_launch<8>(a, st);
+        case 16: return quantize_launch<16>(a, st);
+        case 32: return quantize_launch<32>(a, st);
+        case 64: return quantize_launch<64>(a, st);
+        case 256: return quantize_launch<256>(a, st);
+        default: return quantize_launch<1024>(a, st);
+    }
 }
 
 }  // namespace hb
