@@ -633,7 +633,7 @@ static hb_status norm_launch(const NormArgs& a, const NormPlan& plan, hipStream_
         return launch_status();
     }
     const int64_t wgs = (int64_t)a.N * plan.blocks * plan.chunks, apply_wgs = (int64_t)a.N * plan.blocks * plan.apply_chunks;
-    if (!launch_holds((double)wgs, plan.threads) || !launch_holds((double)apply_wgs, plan.threads) || !launch_holds((double)a.N * a.G, 64)) return HB_ERR_UNSUPPORTED;
+    if (!launch_holds((double)wgs, plan.threads) || !launch_holds((double)apply_wgs, plan.threads) || (plan.join && !launch_holds((double)a.N * a.G, 64))) return HB_ERR_UNSUPPORTED;
     const int lds = 3 * plan.threads * E * 4;
     auto stats = plan.threads <= 256 ? norm_stats_kernel<X, FULL, KIND, 256> : norm_stats_kernel<X, FULL, KIND, kNormThreads>;
     if (lds > 65536)
