@@ -623,14 +623,22 @@ static hb_status norm_launch(const NormArgs& a, const NormPlan& plan, hipStream_
     constexpr int E = kNormEntries<KIND, NormVec<X>::V>;
     constexpr bool ONE = KIND == kNormOne;
     if (plan.slab) {
-        const int64_t wgs = (int64_t)((a.N - 1) / plan.images + 1) * plan.blocks;
-        if (!launch_holds((double)wgs, plan.threads)) return HB_ERR_UNSUPPORTED;
         const int lds = (2 * plan.threads * E + 2 * plan.images * plan.groups) * 4;
         auto kernel = plan.passes <= 1 ? norm_slab_kernel<X, O, 1, FULL, KIND> : plan.passes <= 4 ? norm_slab_kernel<X, O, 4, FULL, KIND> : norm_slab_kernel<X, O, norm_slots(NormVec<X>::V, ONE), FULL, KIND>;
         if (lds > 65536)
             if (hb_status s = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds)) return s;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(plan.threads), lds, st, a);
-        return launch_status();
+        // a launch has fewer than 2^32 lanes: so many images
+        const int64_t most = 0xffffffffll / plan.threads / plan.blocks * plan.images;
+        if (most < 1) return HB_ERR_UNSUPPORTED;
+        for (int64_t n = 0; n < a.N; n += most) {
+            NormArgs part = a;
+            part.x = static_cast<const X*>(a.x) + n * a.x_image;
+            part.out = static_cast<O*>(a.out) + n * a.out_image;
+            part.N = (int)(a.N - n < most ? a.N - n : most);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(((part.N - 1) / plan.images + 1) * plan.blocks)), dim3(plan.threads), lds, st, part);
+            if (hb_status s = launch_status()) return s;
+        }
+        return HB_OK;
     }
     const int64_t wgs = (int64_t)a.N * plan.blocks * plan.chunks, apply_wgs = (int64_t)a.N * plan.blocks * plan.apply_chunks;
     if (!launch_holds((double)wgs, plan.threads) || !launch_holds((double)apply_wgs, plan.threads) || (plan.join && !launch_holds((double)a.N * a.G, 64))) return HB_ERR_UNSUPPORTED;
