@@ -257,7 +257,7 @@ __device__ __forceinline__ void norm_with(int act, F f) {
 // ---------------------------------------------------------------------------
 // Groups whose pixels fit the registers of a workgroup: x is read once, the mean and then the squares of the differences from it are added up in registers, over
 // the lanes through LDS, and the results leave.
-// 8 x 4096 x 1024 in 32 groups, 256 slabs of 256 KB, one to a compute unit: 32.8 us, 4.1 TB/s; all of them read (13 us), then all write (11).  Slabs that share a compute unit
+// 8 x 4096 x 1024 in 32 groups, 256 slabs of 256 KB, one to a compute unit: 32.8 us, 4.1 TB/s (fp32 results 54 us, 3.7); all of them read (13 us), then all write (11).  Slabs that share a compute unit
 // overlap the two, but a group is not divided: what is joined over workgroups is read twice.  1 x 64 x 512, silu: 4.4 us, the launch and a chain of latencies.
 template <class X, class O, int SLOTS, bool FULL, NormKind KIND>
 __global__ void __launch_bounds__(kNormThreads) norm_slab_kernel(NormArgs p) {
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_slab_kernel(NormArgs p) {
 // of its own or, where they are few, by every workgroup of the next; and the rows are read once more.  Every joining takes the means first and the squares about the joint
 // mean, so that no digits are lost where a mean is far from zero.
 // Bound by memory: 1 x 2^20 x 64 in 32 groups, silu, 84.3 us: 40 for the first reading (29 where no results of a call before it are still on their way to memory), 5 for the joining, 41 for
-// the second reading and the results, 6.2 TB/s.  Small maps by the latencies of two launches: 3 x 1079 x 180 fp32, 12 groups, 10.1 us.
+// the second reading and the results, 6.2 TB/s.  fp32 to fp32 163 us; 8 x 4096 x 1024, of which no group fits in fp32, 80 us.  Small maps by the latencies of two launches: 3 x 1079 x 180 fp32, 12 groups, 10.1 us.
 
 // U rows of a lane from `row` on, as many as there are before `end`: their vectors, and how many.
 template <class X, bool FULL, int U>

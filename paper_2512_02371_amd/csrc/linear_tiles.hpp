@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(64 * (BM / WM) * (BN / WN), 1) linear_mfma_ker
 // after tile, and the first two stages of the next tile are copied while the last one's results leave.
 // 8192 x 8192, K 2048 with gelu_tanh: 243 us, 1.13 PFLOP/s at the 2.2 GHz that its power leaves, the matrix units busy for 0.48 of the time (tiles
 // of 128 x 128 280 us); 4096 x 4096, K 4096 111 us (131), K 2048 61 (69), K 1024 35 (40).  Each round of tiles costs some 9 us beside its products.
-// Of integers 8192 x 8192, K 2048 with gelu_tanh: 138 to 143 us, 1.93 to 1.99 POPS, 95 of them products and the rest four epilogues, 22 of that the results at the memory's rate; K 8192 without
+// Of integers 8192 x 8192, K 2048 with gelu_tanh: 138 to 148 us on one card and another, 1.86 to 1.99 POPS (163 us with fp32 output), some 95 of them products and the rest four epilogues, 22 of that the results at the memory's rate; K 8192 without
 // an activation 434 to 450 us, 2.4 to 2.5 POPS; 32768 x 1024, K 1024 with a residual 60.6 to 62.8 us, products 27 and memory 34, one after the other.
 constexpr int kLinLargeLds = 160 * 1024;                                    // two stages of 64 KB and 8 KB of patch a wave
 template <class Op, class O>

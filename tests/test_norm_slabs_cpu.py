@@ -3,7 +3,7 @@ import random
 
 import pytest
 
-from featureforms import Plans
+from featureforms import NORM_FORMS, Plans, norm_form
 from normslabs import NORM_SLABS, first_pixels, slab_form
 
 
@@ -42,3 +42,19 @@ def test_first_vectors_are_a_16th_of_all(plans):
     """What bounds the squares about their mean."""
     for call in NORM_SLABS:
         assert 16 * call[6] >= call[1], call
+
+
+def test_no_form_of_any_kernel_is_left_over(plans):
+    """Those that stream among them, whose calls are featureforms.NORM_FORMS."""
+    rng, calls = random.Random(8), []
+    size = lambda most: max(1, int(most ** rng.random()))
+    while len(calls) < 100000:
+        G = rng.choice([1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 5, 7, 64, size(300)])
+        C = G * (size(4096) if rng.random() < 0.3 else size(128))
+        N, P = size(1 << 16) if rng.random() < 0.3 else size(64), size(1 << 21)
+        if N * P * C <= 1 << 25:
+            calls.append((N, P, C, G, int(rng.random() < 0.5), int(rng.random() < 0.6)))
+    listed = NORM_FORMS + [c[:6] for c in NORM_SLABS]
+    tested = {norm_form(c, p) for c, p in zip(listed, plans.group_norm(listed))}
+    reached = {norm_form(c, p): c for c, p in zip(calls, plans.group_norm(calls))}
+    assert not {f: c for f, c in reached.items() if f not in tested}
